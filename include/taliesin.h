@@ -83,11 +83,15 @@ extern "C" {
 #define TL_DTYPE_F16 2
 #define TL_DTYPE_F32 3
 #define TL_DTYPE_FP8 4
+#define TL_DTYPE_FP8_SCALED 5 /* e4m3 codes with a scale per page and head: see tl_append */
 
 /* KV geometry. Per layer, the K and the V cache are each
  * [pages][page_tokens][n_kv_heads][head_dim] elements; one page of one layer's
  * K (or V) is a "slab" of page_tokens*n_kv_heads*head_dim*elem bytes, which
- * must be a multiple of 1024. */
+ * must be a multiple of 1024. With TL_DTYPE_FP8_SCALED a slab is the codes
+ * [page_tokens][n_kv_heads][head_dim], then a scale byte per head, then padding
+ * to the next multiple of 1024: saves and restores carry the scales with the
+ * codes. */
 typedef struct tl_layout {
   uint32_t n_layers;   /* 1..TL_MAX_LAYERS */
   uint32_t n_kv_heads;
@@ -472,6 +476,108 @@ int tl_chain_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_ch
                    uint32_t* d_tokens_out, uint32_t* d_n_tokens_out, const int32_t* d_tables_in,
                    int32_t* d_tables_out);
 
+/* ---- operators on the paged cache -----------------------------------------
+ * What an engine runs next to the restore: the new tokens of a batch of
+ * requests are appended to the cache's pages (tl_append) and attend to it
+ * (tl_attend), a layer at a time. Both take TL_DTYPE_BF16 and
+ * TL_DTYPE_FP8_SCALED contexts with head_dim 64, 128 or 256 (TL_ELAYOUT for
+ * others), pages of any number of tokens, and one batch:
+ *
+ * Request r of the batch owns rows [d_row_off[r], d_row_off[r + 1]) of every
+ * row tensor (its new tokens, at least 0), and its cache holds d_kv_len[r]
+ * tokens, the new ones among them: its row i stands at position
+ * d_kv_len[r] - rows + i, and position p is row p % page_tokens of page
+ * d_tables[group(layer)][r][p / page_tokens]. All three arrays are read on the
+ * device when the kernels run: a call can be captured into a HIP graph, and
+ * replayed with other contents. Offsets are clamped to n_rows and lengths to
+ * what a table row can address, so inconsistent arrays give fewer rows or keys,
+ * never an access outside the arrays; offsets have to ascend. Rows that no
+ * request owns are not written. */
+typedef struct tl_batch {
+  uint64_t n_reqs;            /* fewer than 2^20 */
+  uint64_t n_rows;            /* rows of the row tensors, fewer than 2^24 */
+  const uint32_t* d_row_off;  /* device [n_reqs + 1], ascending from 0 */
+  const uint32_t* d_kv_len;   /* device [n_reqs] */
+  const int32_t* d_tables;    /* device [n_groups][n_reqs][table_width] page ids */
+  uint64_t table_width;       /* pages of a table row, fewer than 2^28 */
+} tl_batch;
+
+/* Rows of heads, bf16: element d of head h of row t is
+ * d_rows[t * row_stride + h * head_stride + d]. Strides are in elements and
+ * multiples of 8, d_rows is 16-byte aligned: the queries, keys and values may be
+ * slices of one projection's output. Results (tl_attend's out, tl_append's
+ * q_out) must not overlap themselves (TL_EINVAL). */
+typedef struct tl_rows {
+  const void* d_rows;
+  int64_t row_stride;
+  int64_t head_stride;
+} tl_rows;
+
+/* Rotary positions. Pair i of a head's first rot_dim elements (elements i and
+ * i + rot_dim / 2, with TL_ROPE_ADJACENT 2i and 2i + 1) is turned by the angle
+ * whose cosine and sine are d_cos_sin[row][i]: (a, b) becomes
+ * (a cos - b sin, b cos + a sin) in 32-bit arithmetic, every operation rounded.
+ * The row is the token's position on the axis pair_axis[i]: one axis for text,
+ * three (time, height, width) for images and video. */
+#define TL_ROPE_MAX_AXES 3
+#define TL_ROPE_ADJACENT 1
+typedef struct tl_rope {
+  const float* d_cos_sin;   /* device [n_angles][rot_dim / 2][2], 16-byte aligned */
+  int64_t n_angles;
+  const int32_t* d_pos;     /* device [n_axes][n_rows] positions; NULL (one axis):
+                               the token's position in its request */
+  uint32_t rot_dim;         /* a multiple of 16, at most head_dim */
+  uint32_t n_axes;          /* 1 .. TL_ROPE_MAX_AXES */
+  const uint8_t* pair_axis; /* host [rot_dim / 2]: the axis of each pair; NULL
+                               (one axis): 0 */
+  uint32_t flags;           /* 0 or TL_ROPE_ADJACENT */
+} tl_rope;
+
+/* Rotates the new tokens' keys (rope NULL: as they are) and writes keys and
+ * values into the pages of layer `layer`; with q, rotates the n_q_heads query
+ * heads into q_out too (which may be q itself). One kernel, no workspace.
+ *
+ * bf16 pages get the values rounded. Scaled 8-bit pages: K and V of one page
+ * and head share one power-of-two scale, 2^(b - 127) for scale byte b, and an
+ * element is its e4m3 code times the scale. The call takes the smallest b >= 10
+ * that brings the largest finite value that it writes there to 448 or less, or
+ * the page's own b if that is larger and the call does not write the page's row
+ * 0 (a page whose row 0 is written starts afresh); when b rises, the rows before
+ * the first one that is written are rounded again. Values that are not finite
+ * become NaN codes. Powers of two make the scaling exact: a value is rounded to
+ * e4m3 once, and a second time only below the smallest normal code after a rise.
+ *
+ * d_status (device [n_rows] or NULL): TL_ACCEPT for each row, or TL_BADARG for a
+ * row that no request owns, whose position is negative or has no place in the
+ * table, or whose page id is outside [0, n_pages) (nothing is written to the
+ * cache for these), or whose position has no angle (its key, value and query are
+ * written as zeros). Rows of one call must not name one place twice, nor one
+ * page from two requests. */
+int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
+              const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
+              const tl_cache* cache, uint8_t* d_status);
+
+/* Attention of every row over its request's cached keys and values:
+ * out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale * q . k_j), over the keys
+ * j at positions up to the row's own, and above its own minus the layer's window
+ * where the context gives it one; with TL_ATTEND_ALL over all d_kv_len keys (an
+ * encoder's states, whose number is not tied to the rows'), without a window.
+ * Query head h reads K/V head h / (n_q_heads / n_kv_heads). Keys on pages whose
+ * id is outside [0, n_pages), such as -1 for pages that were not restored, are
+ * left out, and what a page holds past the request's keys is not used. A row
+ * that sees no key gets zeros. d_lse (device [n_rows][n_q_heads] floats, or
+ * NULL) gets log(sum_j w_j), minus infinity for such a row.
+ * A value that is NaN or infinite may reach every row of a call that shares its
+ * request, not only those that see it.
+ * Two kernels, no memset and no allocation. d_workspace: device, 16-byte
+ * aligned, tl_attend_workspace_bytes(...) of it; needs no initialisation, and
+ * calls that overlap need separate ones. out must not overlap q. */
+#define TL_ATTEND_ALL 1
+size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t n_reqs, size_t n_rows);
+int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
+              const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
+              float* d_lse, void* d_workspace, size_t workspace_bytes);
+
 /* ---- record files: the disk tier ------------------------------------------
  * Records of one context kept back to back in one file (record id i at byte
  * offset i * record_bytes). Batches of whole records move between the file
@@ -515,7 +621,10 @@ int tl_file_drop_cache(tl_file* f);
 #define TL_KERNEL_CHAIN 5 /* tl_chain_lookup */
 #define TL_KERNEL_STAGE 6 /* tl_chain_stage */
 #define TL_KERNEL_INDEX 7 /* every tl_dindex_* kernel */
-#define TL_KERNEL_COUNT 8
+#define TL_KERNEL_APPEND 8
+#define TL_KERNEL_ATTEND 9
+#define TL_KERNEL_ATTEND_JOIN 10
+#define TL_KERNEL_COUNT 11
 int tl_timing(int enable);
 int tl_timing_read(int kernel, double* total_ms, uint64_t* count);
 

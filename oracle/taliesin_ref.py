@@ -67,7 +67,7 @@ META_ALIGN = 256
 ROOT_OFFSET = 144
 NS_TAG = b"taliesin-ns-v1"
 
-DTYPE_BYTES = {1: 2, 2: 2, 3: 4, 4: 1}  # bf16, f16, f32, fp8
+DTYPE_BYTES = {1: 2, 2: 2, 3: 4, 4: 1, 5: 1}  # bf16, f16, f32, fp8, fp8 with a scale per page and head
 MAX_LAYERS = 256
 MAX_GROUPS = 8
 MAX_PAGES_PER_BLOCK = 1 << 16
@@ -109,7 +109,7 @@ class Layout:
     n_layers: int
     n_kv_heads: int
     head_dim: int
-    dtype: int  # 1 bf16, 2 f16, 3 f32, 4 fp8
+    dtype: int  # 1 bf16, 2 f16, 3 f32, 4 fp8, 5 scaled fp8
     page_tokens: int
     layer_window: Tuple[int, ...] = ()
     layer_group: Tuple[int, ...] = ()
@@ -145,8 +145,10 @@ class Layout:
 
     @property
     def slab_bytes(self):
-        """Bytes of one (layer, K|V) page: P * H * D * element size."""
-        return self.page_tokens * self.n_kv_heads * self.head_dim * DTYPE_BYTES[self.dtype]
+        """Bytes of one (layer, K|V) page: P * H * D * element size; scaled
+        fp8: one more byte per head, and padding to whole rows."""
+        n = self.page_tokens * self.n_kv_heads * self.head_dim * DTYPE_BYTES[self.dtype]
+        return -(-(n + self.n_kv_heads) // ROW_BYTES) * ROW_BYTES if self.dtype == 5 else n
 
     @property
     def n_slabs(self):

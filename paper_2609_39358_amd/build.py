@@ -4,6 +4,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -15,7 +16,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 
 HIP_FLAGS = [
     "-O3", "-fPIC", "-std=c++17", "--offload-arch=gfx950",
-    # no packed FP32 instructions anywhere (the kernels do no FP32 math)
+    # no packed FP32 instructions anywhere
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
@@ -39,15 +40,16 @@ def build(verbose: bool = False, extra_hip_flags=(), out: str = OUT, build_dir: 
     cxx = os.environ.get("CXX") or shutil.which("g++") or "g++"
     os.makedirs(build_dir, exist_ok=True)
     inc = ["-I", INCLUDE, "-I", CSRC]
-    objs = []
-    for src in ("ctx.cpp", "sha256.cpp", "file_io.cpp"):
-        o = os.path.join(build_dir, src + ".o")
-        _run([cxx, *CXX_FLAGS, *inc, "-c", os.path.join(CSRC, src), "-o", o], verbose)
-        objs.append(o)
-    for src in ("kernels.hip", "chain.hip"):
-        o = os.path.join(build_dir, src + ".o")
-        _run([hipcc, *HIP_FLAGS, *extra_hip_flags, *inc, "-c", os.path.join(CSRC, src), "-o", o], verbose)
-        objs.append(o)
+    sources = ("ctx.cpp", "sha256.cpp", "file_io.cpp", "operators.cpp", "kernels.hip", "chain.hip", "append.hip", "attend.hip")
+    obj = lambda src: os.path.join(build_dir, src + ".o")  # noqa: E731
+
+    def compile_one(src):
+        how = [hipcc, *HIP_FLAGS, *extra_hip_flags] if src.endswith(".hip") else [cxx, *CXX_FLAGS]
+        _run([*how, *inc, "-c", os.path.join(CSRC, src), "-o", obj(src)], verbose)
+
+    with ThreadPoolExecutor(4) as pool:
+        list(pool.map(compile_one, sources))
+    objs = [obj(src) for src in sources]
     tmp = out + ".tmp"
     _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp, *objs], verbose)
     os.replace(tmp, out)

@@ -19,6 +19,7 @@ uint32_t elem_bytes(uint32_t dtype) {
     case TL_DTYPE_F16: return 2;
     case TL_DTYPE_F32: return 4;
     case TL_DTYPE_FP8: return 1;
+    case TL_DTYPE_FP8_SCALED: return 1;
     default: return 0;
   }
 }
@@ -34,7 +35,8 @@ int make_geometry(const tl_layout* lay, tl::Geo* g) {
   if (ppb > tl::kMaxPagesPerBlock) return TL_ELAYOUT;
   const uint32_t e = elem_bytes(lay->dtype);
   if (!e) return TL_ELAYOUT;
-  // slab = P*H*D*e, guarded against overflow; at most 2^31 bytes
+  // slab = P*H*D*e, guarded against overflow; at most 2^31 bytes. Scaled
+  // 8-bit pages: the codes, a scale byte per head and padding to whole rows.
   const uint64_t lim = 1ull << 31;
   uint64_t slab = lay->page_tokens;
   if (slab > lim) return TL_ELAYOUT;
@@ -43,6 +45,8 @@ int make_geometry(const tl_layout* lay, tl::Geo* g) {
   slab *= lay->head_dim;
   if (slab > lim) return TL_ELAYOUT;
   slab *= e;
+  if (lay->dtype == TL_DTYPE_FP8_SCALED)
+    slab = (slab + lay->n_kv_heads + tl::kRowBytes - 1) / tl::kRowBytes * tl::kRowBytes;
   if (slab > lim || slab % tl::kRowBytes) return TL_ELAYOUT;
   memset(g, 0, sizeof *g);
   g->n_layers = lay->n_layers;

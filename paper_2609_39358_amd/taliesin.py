@@ -22,7 +22,7 @@ LIB_PATH = os.environ.get("TALIESIN_LIB") or os.path.join(_HERE, "libtaliesin.so
 TL_OK, TL_EINVAL, TL_ELAYOUT, TL_ENOIDENT, TL_EDEVICE, TL_ENOMEM, TL_EFULL, TL_ERANGE, TL_EIO = 0, -1, -2, -3, -4, -5, -6, -7, -8
 ACCEPT, MISSING, BADARG, TRUNCATED, OVERLONG = 0x01, 0x10, 0x11, 0x12, 0x13
 ROOT, HEADER, POSITION, KEY, TOKENS, SEGMENT = 0x14, 0x15, 0x16, 0x17, 0x18, 0x19
-DTYPE = {"bf16": 1, "f16": 2, "f32": 3, "fp8": 4}
+DTYPE = {"bf16": 1, "f16": 2, "f32": 3, "fp8": 4, "fp8_scaled": 5}
 KEY_BYTES = 32
 
 
@@ -64,6 +64,21 @@ class tl_chains(ctypes.Structure):
                 ("d_tok_off", ctypes.c_void_p), ("d_slot_off", ctypes.c_void_p),
                 ("n_slots", ctypes.c_uint64), ("d_parents", ctypes.c_void_p),
                 ("d_first_block", ctypes.c_void_p)]
+
+
+class tl_batch(ctypes.Structure):
+    _fields_ = [("n_reqs", ctypes.c_uint64), ("n_rows", ctypes.c_uint64), ("d_row_off", ctypes.c_void_p),
+                ("d_kv_len", ctypes.c_void_p), ("d_tables", ctypes.c_void_p), ("table_width", ctypes.c_uint64)]
+
+
+class tl_rows(ctypes.Structure):
+    _fields_ = [("d_rows", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class tl_rope(ctypes.Structure):
+    _fields_ = [("d_cos_sin", ctypes.c_void_p), ("n_angles", ctypes.c_int64), ("d_pos", ctypes.c_void_p),
+                ("rot_dim", ctypes.c_uint32), ("n_axes", ctypes.c_uint32), ("pair_axis", ctypes.c_void_p),
+                ("flags", ctypes.c_uint32)]
 
 
 def _load():
@@ -111,6 +126,12 @@ def _load():
         "tl_block_fingerprints": (c.c_int, [P, P, c.c_size_t, P, P, P, P]),
         "tl_chain_lookup_par": (c.c_int, [P, P, c.c_size_t, c.POINTER(tl_chains), P, P, P, c.c_uint64, c.c_uint32,
                                           P, P, P]),
+        "tl_append": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.POINTER(tl_rope), c.POINTER(tl_rows),
+                                c.POINTER(tl_rows), c.c_uint32, c.POINTER(tl_rows), c.POINTER(tl_rows),
+                                c.POINTER(tl_cache), P]),
+        "tl_attend_workspace_bytes": (c.c_size_t, [P, c.c_uint32, c.c_size_t, c.c_size_t]),
+        "tl_attend": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.c_uint32, c.POINTER(tl_rows),
+                                c.POINTER(tl_cache), c.c_float, c.c_uint32, c.POINTER(tl_rows), P, P, c.c_size_t]),
         "tl_file_open": (P, [c.c_char_p, c.c_uint64, c.c_int, c.c_int, c.POINTER(c.c_int)]),
         "tl_file_close": (c.c_int, [P]),
         "tl_file_records": (c.c_uint64, [P]),
@@ -139,12 +160,13 @@ EXPORTED = (
     "tl_index_destroy", "tl_index_put", "tl_index_get_batch", "tl_index_size", "tl_index_lookup_prefix",
     "tl_dindex_bytes", "tl_dindex_create", "tl_dindex_destroy", "tl_dindex_workspace_bytes",
     "tl_dindex_put", "tl_dindex_get", "tl_dindex_stats", "tl_chain_lookup", "tl_chain_stage",
-    "tl_block_fingerprints", "tl_chain_lookup_par", "tl_file_open", "tl_file_close", "tl_file_records",
+    "tl_block_fingerprints", "tl_chain_lookup_par", "tl_append", "tl_attend_workspace_bytes", "tl_attend",
+    "tl_file_open", "tl_file_close", "tl_file_records",
     "tl_file_read", "tl_file_write", "tl_file_drop_cache",
     "tl_status_string", "tl_verdict_string", "tl_abi_version", "tl_test_sha256", "tl_timing",
     "tl_timing_read")
 KERNELS = {"save_seg": 0, "save_meta": 1, "load_init": 2, "load_main": 3, "load_final": 4, "chain": 5,
-           "stage": 6, "index": 7}
+           "stage": 6, "index": 7, "append": 8, "attend": 9, "attend_join": 10}
 TL_INDEX_STORED, TL_INDEX_FULL, TL_INDEX_TAG_CLASH = 0x01, 0x20, 0x21
 TL_CHAIN_ALL_KEYS, TL_CHAIN_TAIL = 1, 2
 TL_KEYS_TAIL = 1
@@ -192,8 +214,9 @@ def _check(st: int, what: str):
 class Ctx:
     """Owns a tl_ctx*. Geometry fields mirror tl_geometry."""
 
-    def __init__(self, handle: int):
+    def __init__(self, handle: int, n_kv_heads: int = 0, head_dim: int = 0):
         self._h = handle
+        self.n_kv_heads, self.head_dim = n_kv_heads, head_dim
         g = tl_geometry()
         _check(_lib.tl_ctx_geometry(handle, ctypes.byref(g)), "tl_ctx_geometry")
         for name, _ in tl_geometry._fields_:
@@ -233,7 +256,7 @@ def tl_ctx_create(tenant: bytes, model_fp: bytes, n_layers: int, n_kv_heads: int
     h = _lib.tl_ctx_create(t, len(t), f, len(f), ctypes.byref(lay), ctypes.byref(st))
     if not h:
         raise TaliesinError(st.value, "tl_ctx_create")
-    return Ctx(h)
+    return Ctx(h, n_kv_heads, head_dim)
 
 
 def tl_ns_digest(ctx: Ctx) -> bytes:
@@ -539,6 +562,101 @@ def tl_chain_stage(ctx: Ctx, stream, n_chains: int, chains: tl_chains, d_hits, d
                                _addr(d_record_ptrs), _addr(d_record_lens), _addr(d_block_index),
                                _addr(d_tokens_out), _addr(d_n_tokens_out), _addr(d_tables_in),
                                _addr(d_tables_out)), "tl_chain_stage")
+
+
+# ------------------------------------------------------------------ operators on the paged cache
+TL_ROPE_ADJACENT = 1
+TL_ATTEND_ALL = 1
+
+
+def make_batch(n_reqs: int, n_rows: int, d_row_off, d_kv_len, d_tables, table_width: int) -> tl_batch:
+    """One call's requests (tl_batch): d_row_off u32 [n_reqs + 1], d_kv_len
+    u32 [n_reqs], d_tables i32 [n_groups, n_reqs, table_width], on the device."""
+    _fits(d_row_off, 4 * (n_reqs + 1), "row offsets")
+    _fits(d_kv_len, 4 * n_reqs, "cache lengths")
+    _fits(d_tables, 4 * n_reqs * table_width, "page tables")
+    b = tl_batch(n_reqs, n_rows, _addr(d_row_off), _addr(d_kv_len), _addr(d_tables), table_width)
+    b._keep = (d_row_off, d_kv_len, d_tables)
+    return b
+
+
+def make_rope(d_cos_sin, rot_dim: int, d_pos=None, pair_axis: Optional[Sequence[int]] = None,
+              adjacent: bool = False) -> tl_rope:
+    """Rotary positions (tl_rope): d_cos_sin f32 [n_angles, rot_dim / 2, 2];
+    d_pos i32 [n_axes, n_rows] or [n_rows], or None for the tokens' places in
+    their requests; pair_axis: the axis of each of the rot_dim / 2 pairs."""
+    if pair_axis is not None and len(pair_axis) != rot_dim // 2:
+        raise ValueError("%d axes for %d pairs" % (len(pair_axis), rot_dim // 2))
+    n_angles = d_cos_sin.shape[0]
+    _fits(d_cos_sin, 4 * n_angles * rot_dim, "angles")
+    n_axes = 1 if d_pos is None or d_pos.dim() == 1 else d_pos.shape[0]
+    axis = None
+    if pair_axis is not None:
+        axis = (ctypes.c_uint8 * len(pair_axis))(*pair_axis)
+    r = tl_rope(_addr(d_cos_sin), n_angles, _addr(d_pos), rot_dim, n_axes,
+                None if axis is None else ctypes.cast(axis, ctypes.c_void_p), TL_ROPE_ADJACENT if adjacent else 0)
+    r._keep = (d_cos_sin, d_pos, axis)
+    return r
+
+
+def _rows(x, batch: tl_batch, dim: Optional[int], what: str) -> tl_rows:
+    """A bf16 device tensor [n_rows, heads, head_dim] whose last dimension is
+    contiguous; any other strides that are multiples of 8."""
+    if x.dtype.itemsize != 2 or "bfloat16" not in str(x.dtype):
+        raise ValueError("%s must be bf16, got %s" % (what, x.dtype))
+    if x.device.type != "cuda":
+        raise ValueError("%s must be device memory, got a %s tensor" % (what, x.device.type))
+    if x.dim() != 3 or x.shape[0] != batch.n_rows or (dim is not None and x.shape[2] != dim):
+        raise ValueError("%s has shape %s for %d rows" % (what, tuple(x.shape), batch.n_rows))
+    if x.stride(2) != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % what)
+    return tl_rows(x.data_ptr(), x.stride(0), x.stride(1))
+
+
+def _check_operator(ctx: Ctx, batch: tl_batch, cache: tl_cache):
+    keep = getattr(batch, "_keep", None)
+    if keep is not None:
+        _fits(keep[2], 4 * ctx.n_groups * batch.n_reqs * batch.table_width, "page tables")
+    _check_cache(ctx, cache)
+
+
+def tl_append(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, k, v, rope: Optional[tl_rope] = None,
+              q=None, q_out=None, d_status=None):
+    """Rotates and appends the rows' keys and values [n_rows, n_kv_heads,
+    head_dim] to the cache's pages, and rotates the queries q into q_out."""
+    _check_operator(ctx, batch, cache)
+    if k.shape[1] != ctx.n_kv_heads or v.shape[1] != ctx.n_kv_heads:
+        raise ValueError("keys and values of %d and %d heads for a cache of %d" % (k.shape[1], v.shape[1], ctx.n_kv_heads))
+    if (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
+        raise ValueError("queries and rotated queries go together and have one shape")
+    _fits(d_status, batch.n_rows, "status")
+    if rope is not None and getattr(rope, "_keep", None) is not None:
+        _fits(rope._keep[1], 4 * rope.n_axes * batch.n_rows, "positions")
+    rows = lambda x, what: None if x is None else ctypes.byref(_rows(x, batch, ctx.head_dim, what))  # noqa: E731
+    _check(_lib.tl_append(ctx.handle, _stream(stream), layer, ctypes.byref(batch),
+                          None if rope is None else ctypes.byref(rope), rows(k, "keys"), rows(v, "values"),
+                          0 if q is None else q.shape[1], rows(q, "queries"), rows(q_out, "rotated queries"),
+                          ctypes.byref(cache), _addr(d_status)), "tl_append")
+
+
+def tl_attend_workspace_bytes(ctx: Ctx, n_q_heads: int, n_reqs: int, n_rows: int) -> int:
+    return int(_lib.tl_attend_workspace_bytes(ctx.handle, n_q_heads, n_reqs, n_rows))
+
+
+def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q, out, d_workspace, workspace_bytes: int,
+              scale: Optional[float] = None, lse=None, all_keys: bool = False):
+    """Attention of q [n_rows, n_q_heads, head_dim] over the cache into out;
+    scale: head_dim ** -0.5 by default; all_keys: TL_ATTEND_ALL."""
+    _check_operator(ctx, batch, cache)
+    if q.shape != out.shape:
+        raise ValueError("queries %s and results %s differ in shape" % (tuple(q.shape), tuple(out.shape)))
+    _fits(lse, 4 * batch.n_rows * q.shape[1], "lse")
+    _fits(d_workspace, workspace_bytes, "workspace")
+    _check(_lib.tl_attend(ctx.handle, _stream(stream), layer, ctypes.byref(batch), q.shape[1],
+                          ctypes.byref(_rows(q, batch, ctx.head_dim, "queries")), ctypes.byref(cache),
+                          ctx.head_dim ** -0.5 if scale is None else scale, TL_ATTEND_ALL if all_keys else 0,
+                          ctypes.byref(_rows(out, batch, ctx.head_dim, "results")), _addr(lse), _addr(d_workspace),
+                          workspace_bytes), "tl_attend")
 
 
 # ------------------------------------------------------------------ record files (disk tier)
