@@ -11,18 +11,27 @@
 // The matrix instructions take bf16. A code times its power-of-two scale is a
 // bf16 value exactly; the weights 2^(s - m) are rounded to bf16 for the product
 // with v (as accurate as the bf16 output), and not for the sum.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace tl {
 
-// The part of an item that one worker left to others: see k_attend_join.
+// What the joining kernel has to know of a worker's first tile.
 struct Share {
-  uint64_t first, end;  // units of the item
-  uint64_t total;       // units of the call
-  uint32_t workers;
-  uint32_t r, head, tile;
-  uint32_t open;        // the worker's first segment goes on with an item that another began
-  uint32_t pad;
+  uint32_t parts;  // workers of the tile, this one the second of them; 0: nothing to join here
+  uint32_t kind, head, tile;
+  uint32_t row0, rows;  // of the request
+};
+
+// How requests are cut into tiles: of 16 rows, or of 32 for each wavefront.
+struct Kind {
+  uint32_t rows;               // of a tile
+  uint32_t parts, part_heads;  // a K/V head's query heads in `parts` runs of at most part_heads
+  uint32_t tile_rows;          // batch rows of a tile: floor(rows / part_heads)
+  uint32_t heads_shift;        // log2 of the runs that a workgroup takes together
+  uint32_t heads;              // how many times it does so for a batch row's heads
+  uint32_t block_shift;        // log2 of the keys of a block
 };
 
 struct AttendArgs {
@@ -32,69 +41,72 @@ struct AttendArgs {
   int64_t q_token, q_head;
   uint16_t* out;
   int64_t o_token, o_head;
-  float* lse;  // [rows][query heads] or null
-  uint32_t n_heads, group;      // K/V heads, query heads of each
-  uint32_t parts, part_heads;   // a K/V head's query heads in `parts` runs of at most part_heads
-  uint32_t tile_rows;           // batch rows of a tile: floor(M / part_heads)
+  float* lse;                // [rows][query heads] or null
+  uint32_t n_heads, group;   // K/V heads, query heads of each
+  Kind kind[2];
+  uint32_t few;              // requests of at most this many rows are of kind 0
   uint32_t all, window;
-  float scale;                  // times log2(e)
-  Share* share;                 // [workers]
-  float* part_ml;               // [2 * workers][M][2]
-  float* part_o;                // [2 * workers][M][D]
+  float scale;               // times log2(e), above 0
+  uint32_t q_sign;           // flips the signs of q for scales below 0
+  uint32_t slot_rows;        // rows of a worker's part
+  Share* share;              // [workers]
+  float* part_ml;            // [2 * workers][slot_rows][2]
+  float* part_o;             // [2 * workers][slot_rows][D]
 };
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kPlan = 256;  // threads that make a plan
 constexpr float kNone = -__builtin_inff();
 constexpr float kSlack = 8.f;  // how far a block's scores may exceed the running maximum
 
-typedef const __attribute__((address_space(4))) uint32_t* ConstU32;
-
 // ---- which keys a tile sees -----------------------------------------------------
-struct Span {
-  int lo, hi;      // keys [lo, hi) are seen by some row of the tile
-  uint32_t b0, n;  // blocks of KT keys from b0 on; at least one, so that every tile has a worker
-};
-
-template <int KT>
-__device__ __forceinline__ Span span_of(const AttendArgs& a, uint32_t rows, int held, int before, uint32_t tile) {
-  Span s;
-  s.lo = 0;
-  s.hi = held;
-  if (!a.all) {
-    const int t0 = (int)(tile * a.tile_rows), t1 = (int)min(tile * a.tile_rows + a.tile_rows, rows);
-    s.hi = min(held, before + t1);
-    if (a.window) s.lo = (int)max((int64_t)0, (int64_t)before + t0 + 1 - (int64_t)a.window);
-  }
-  s.hi = max(s.hi, 0);
-  s.lo = min(s.lo, s.hi);
-  s.b0 = (uint32_t)s.lo / KT;
-  s.n = max(1u, ((uint32_t)s.hi + KT - 1) / KT - s.b0);
-  return s;
-}
-
 struct Request {
   uint32_t row0, rows, tiles;
   int held, before;  // keys, and keys before the first row's own
+  uint32_t kind, tile_rows, heads, block_shift;  // as in Kind
 };
 
 __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
   Request q;
   q.row0 = a.b.first_row(r);
-  const uint32_t row1 = a.b.first_row(r + 1);
+  const uint32_t row1 = a.b.first_row(r + 1), kv_len = a.b.kv_len[r];
   q.rows = row1 > q.row0 ? row1 - q.row0 : 0;
-  q.tiles = (q.rows + a.tile_rows - 1) / a.tile_rows;
-  q.held = a.c.n_pages ? (int)a.b.held(r) : 0;
-  q.before = (int)min(a.b.kv_len[r], 0x7fffffffu) - (int)q.rows;
+  q.held = a.c.n_pages ? (int)min(kv_len, a.b.most) : 0;
+  q.before = (int)min(kv_len, 0x7fffffffu) - (int)q.rows;
+  q.kind = q.rows > a.few;
+  q.tile_rows = q.kind ? a.kind[1].tile_rows : a.kind[0].tile_rows;
+  q.heads = q.kind ? a.kind[1].heads : a.kind[0].heads;
+  q.block_shift = q.kind ? a.kind[1].block_shift : a.kind[0].block_shift;
+  q.tiles = (q.rows + q.tile_rows - 1) / q.tile_rows;
   return q;
 }
 
+struct Span {
+  int lo, hi;      // keys [lo, hi) are seen by some row of the tile
+  uint32_t b0, n;  // blocks of keys from b0 on; at least one, so that every tile has a worker
+};
+
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, uint32_t tile) {
+  Span s;
+  s.lo = 0;
+  s.hi = q.held;
+  if (!a.all) {
+    const int t0 = (int)(tile * q.tile_rows), t1 = (int)min(tile * q.tile_rows + q.tile_rows, q.rows);
+    s.hi = min(q.held, q.before + t1);
+    if (a.window) s.lo = (int)max((int64_t)0, (int64_t)q.before + t0 + 1 - (int64_t)a.window);
+  }
+  s.hi = max(s.hi, 0);
+  s.lo = min(s.lo, s.hi);
+  s.b0 = (uint32_t)s.lo >> q.block_shift;
+  s.n = s.hi > s.lo ? (((uint32_t)s.hi - 1) >> q.block_shift) + 1 - s.b0 : 1;
+  return s;
+}
+
 // Blocks of a request's tiles tile0, tile0 + step, ...
-template <int KT>
 __device__ __forceinline__ uint64_t blocks_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
   uint64_t n = 0;
-  for (uint32_t t = tile0; t < q.tiles; t += step) n += span_of<KT>(a, q.rows, q.held, q.before, t).n;
+  for (uint32_t t = tile0; t < q.tiles; t += step) n += span_of(a, q, t).n;
   return n;
 }
 
@@ -107,92 +119,107 @@ __device__ __forceinline__ uint64_t blocks_of(const AttendArgs& a, const Request
 struct Cursor {
   uint64_t at, end;  // units left
   uint64_t total;
-  uint32_t workers;
+  uint32_t workers, worker;
   uint32_t r, head, tile;
   uint64_t first;  // first unit of the tile
 };
 
 struct PlanLds {
-  uint64_t sum[kThreads + 1];
-  uint64_t found_at, found_blocks;
+  uint64_t sum[kPlan + 1];
+  uint64_t found_at;
   uint32_t found;
 };
 
-template <int KT>
-__device__ bool plan(const AttendArgs& a, PlanLds& l, uint32_t worker, Cursor& c) {
-  const uint32_t tid = threadIdx.x, n = a.b.n_reqs, heads = a.n_heads * a.parts;
+__device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
+  const uint32_t tid = threadIdx.x, n = a.b.n_reqs;
   // threads for each request (few requests), or requests for each thread
   uint32_t split = 1;
-  while (split < 64 && 2 * split * n <= kThreads) split *= 2;
-  const uint32_t per = (n + kThreads - 1) / kThreads;
+  while (split < 64 && 2 * split * n <= kPlan) split *= 2;
+  const uint32_t per = (n + kPlan - 1) / kPlan;
   uint64_t mine = 0;
   if (split > 1) {
-    const uint32_t r = tid / split;
-    if (r < n) mine = blocks_of<KT>(a, request_of(a, r), tid % split, split);
-  } else {
-    for (uint32_t r = tid * per; r < min(tid * per + per, n); ++r) mine += blocks_of<KT>(a, request_of(a, r), 0, 1);
+    if (tid / split < n) {
+      const Request q = request_of(a, tid / split);
+      mine = blocks_of(a, q, tid % split, split) * q.heads;
+    }
+  } else if (tid < kPlan) {
+    for (uint32_t r = tid * per; r < min(tid * per + per, n); ++r) {
+      const Request q = request_of(a, r);
+      mine += blocks_of(a, q, 0, 1) * q.heads;
+    }
   }
-  mine *= heads;
   uint64_t incl = mine;
   for (uint32_t k = 1; k < 64; k *= 2) {
     const uint64_t up = __shfl_up(incl, k);
     if ((tid & 63) >= k) incl += up;
   }
-  __shared__ uint64_t wave_sum[kThreads / 64];
-  if ((tid & 63) == 63) wave_sum[tid / 64] = incl;
+  __shared__ uint64_t wave_sum[kPlan / 64];
+  if ((tid & 63) == 63 && tid < kPlan) wave_sum[tid / 64] = incl;
   __syncthreads();
-  uint64_t before = 0;
-  for (uint32_t w = 0; w < tid / 64; ++w) before += wave_sum[w];
-  l.sum[tid] = before + incl - mine;
-  if (tid == kThreads - 1) l.sum[kThreads] = before + incl;
+  if (tid < kPlan) {
+    uint64_t before = 0;
+    for (uint32_t w = 0; w < tid / 64; ++w) before += wave_sum[w];
+    l.sum[tid] = before + incl - mine;
+    if (tid == kPlan - 1) l.sum[kPlan] = before + incl;
+  }
   if (tid == 0) l.found = ~0u;
   __syncthreads();
-  c.total = l.sum[kThreads];
+  c.total = l.sum[kPlan];
   c.workers = (uint32_t)min((uint64_t)gridDim.x, c.total);
-  // neighbouring runs of units on the same chiplet, whose workgroups share an L2
-  if (c.workers == gridDim.x && gridDim.x % 8 == 0) worker = worker % 8 * (gridDim.x / 8) + worker / 8;
+  // runs that follow each other go to workgroups of one chiplet, which share an L2
+  c.worker = blockIdx.x;
+  if (c.workers == gridDim.x && gridDim.x % 8 == 0) c.worker = c.worker % 8 * (gridDim.x / 8) + c.worker / 8;
   c.at = c.end = 0;
-  if (worker < c.workers) {
-    c.at = c.total * worker / c.workers;
-    c.end = c.total * (worker + 1) / c.workers;
+  if (c.worker < c.workers) {
+    c.at = c.total * c.worker / c.workers;
+    c.end = c.total * (c.worker + 1) / c.workers;
   }
-  const uint32_t step = split;
-  if (c.at < c.end && tid % step == 0 && l.sum[tid] <= c.at && c.at < l.sum[tid + step]) {
-    l.found = tid / step * (split > 1 ? 1 : per);
+  if (c.at < c.end && tid < kPlan && tid % split == 0 && l.sum[tid] <= c.at && c.at < l.sum[tid + split]) {
+    l.found = tid / split * (split > 1 ? 1 : per);
     l.found_at = l.sum[tid];
   }
   __syncthreads();
   if (l.found == ~0u) return false;
-  c.r = l.found;
+  c.r = __builtin_amdgcn_readfirstlane(l.found);
   c.first = l.found_at;
   while (c.r < n) {
     const Request q = request_of(a, c.r);
-    const uint64_t blocks = split > 1 ? (l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / heads : blocks_of<KT>(a, q, 0, 1);
-    if (c.at < c.first + blocks * heads) {
+    const uint64_t blocks = split > 1 ? (l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : blocks_of(a, q, 0, 1);
+    if (c.at < c.first + blocks * q.heads) {
       c.head = (uint32_t)((c.at - c.first) / blocks);
       c.first += c.head * blocks;
       c.tile = 0;
       for (;;) {
-        const uint32_t k = span_of<KT>(a, q.rows, q.held, q.before, c.tile).n;
+        const uint32_t k = span_of(a, q, c.tile).n;
         if (c.at < c.first + k) return true;
         c.first += k;
         ++c.tile;
       }
     }
-    c.first += blocks * heads;
+    c.first += blocks * q.heads;
     ++c.r;
   }
   return false;
 }
 
-// The tile after (r, head, tile); its first unit is c.first.
-__device__ __forceinline__ void next_tile(const AttendArgs& a, Cursor& c) {
-  if (++c.tile < request_of(a, c.r).tiles) return;
+// The tile after the cursor's; its first unit is c.first.
+__device__ __forceinline__ void next_tile(const AttendArgs& a, const Request& q, Cursor& c) {
+  if (++c.tile < q.tiles) return;
   c.tile = 0;
-  if (++c.head < a.n_heads * a.parts) return;
+  if (++c.head < q.heads) return;
   c.head = 0;
   while (++c.r < a.b.n_reqs && request_of(a, c.r).tiles == 0) {
   }
+}
+
+// A worker's first tile, for the joining kernel: worker w's run begins at
+// floor(total * w / workers). The second worker of a tile sees to it.
+__device__ void note_share(const AttendArgs& a, const Cursor& c, const Request& q, const Span& s) {
+  Share sh = {0, q.kind, c.head, c.tile, q.row0, q.rows};
+  const uint64_t end = c.first + s.n;
+  if (c.at > c.first && c.total * (c.worker - 1) < (c.first + 1) * c.workers)
+    sh.parts = (uint32_t)((end * c.workers - 1) / c.total) + 2 - c.worker;
+  a.share[c.worker] = sh;
 }
 
 // ---- one row ------------------------------------------------------------------------
@@ -203,12 +230,12 @@ struct Place {
   int lo, hi;  // it sees keys [lo, hi)
 };
 
-__device__ __forceinline__ Place place_of(const AttendArgs& a, const Request& q, uint32_t head, uint32_t tile, uint32_t m) {
+__device__ __forceinline__ Place place_of(const AttendArgs& a, const Kind& k, const Request& q, uint32_t head, uint32_t tile, uint32_t m) {
   Place p;
-  const uint32_t part = head % a.parts, kv = head / a.parts;
-  const uint32_t tok = m / a.part_heads, g = part * a.part_heads + m % a.part_heads;
-  const uint32_t i = tile * a.tile_rows + tok;
-  p.there = tok < a.tile_rows && i < q.rows && g < a.group;
+  const uint32_t part = head % k.parts, kv = head / k.parts;
+  const uint32_t tok = m / k.part_heads, g = part * k.part_heads + m % k.part_heads;
+  const uint32_t i = tile * k.tile_rows + tok;
+  p.there = tok < k.tile_rows && i < q.rows && g < a.group;
   p.row = q.row0 + (p.there ? i : 0);
   p.head = kv * a.group + (p.there ? g : 0);
   p.lo = 0;
@@ -224,92 +251,6 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Request& q,
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// ---- tiles of 16 rows -----------------------------------------------------------------
-// For few rows per request. Every key and value is used by 16 rows at most, so
-// the cache's bytes are what it costs: they go from memory to registers in the
-// layout that the matrix instructions take, with no stop in shared memory. Each
-// of a workgroup's four wavefronts takes 32 of a block's 128 keys.
-//
-// S^T = K Q^T with mfma 16x16x32: lane l gives key l % 16 and takes row l % 16.
-// Its result holds keys 4 * (l / 16) + i, i < 4, of each half of the 32: the
-// eight weights that the lane gives to O^T = V^T P^T, whose sum over keys runs in
-// that order. For V a lane loads D / 16 neighbouring elements of those eight
-// keys and transposes them in registers: product n takes element n of each.
-constexpr int kBlock16 = 128;
-
-template <int D, bool FP8>
-struct Tile16 {
-  static constexpr int kElems = D / 16;                        // of V per lane and key
-  static constexpr int kKWords = FP8 ? D / 16 : D / 8;         // 32-bit words of K per lane and key
-  static constexpr int kVWords = FP8 ? kElems / 4 : kElems / 2;
-  uint32_t k[2][kKWords];
-  uint32_t v[8][kVWords];
-  float k_scale[2], v_scale[8];
-  uint32_t seen;  // which of the 32 keys are to be used
-};
-
-struct Ids16 {  // of one of 32 keys per lane
-  uint32_t page;
-  uint32_t row;
-  bool in;
-};
-
-__device__ __forceinline__ Ids16 ids16(const AttendArgs& a, const int32_t* table, int key, const Span& s) {
-  Ids16 x;
-  x.in = key >= s.lo && key < s.hi;
-  const uint32_t at = x.in ? (uint32_t)key : 0u, i = a.b.page.div(at);
-  x.row = at - i * a.b.page.d;
-  x.page = (uint32_t)table[i];
-  return x;
-}
-
-template <int D, bool FP8>
-__device__ __forceinline__ void load16(const AttendArgs& a, const uint8_t* kp, const uint8_t* vp, uint32_t kv, const Ids16& id,
-                                       Tile16<D, FP8>& t) {
-  constexpr int kRow = FP8 ? D : 2 * D;  // bytes of a head's row
-  const uint32_t lane = threadIdx.x & 63, c = lane % 16, quad = lane / 16;
-  const bool fine = id.in && id.page < a.c.n_pages;
-  t.seen = (uint32_t)__ballot(fine);
-  // keys that are not to be used are read from page 0
-  const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
-  const int64_t off = page + (fine ? (int64_t)id.row * a.n_heads * kRow : 0) + (int64_t)kv * kRow;
-  uint32_t scale = 127;
-  if (FP8) scale = scale_held((lane < 32 ? kp : vp)[page + a.c.scale_off + kv]);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t at = __shfl(off, h * 16 + c);
-    const uint8_t* p = kp + at + 16 * quad;
-#pragma unroll
-    for (int i = 0; i < Tile16<D, FP8>::kKWords / 4; ++i) {
-      const u32x4 w = *(const u32x4*)(p + 64 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t.k[h][4 * i + j] = w[j];
-    }
-    if (FP8) t.k_scale[h] = scale_value(__shfl(scale, h * 16 + c));
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t key = (i / 4) * 16 + quad * 4 + i % 4;
-    const uint8_t* p = vp + __shfl(off, key) + kRow / 16 * c;
-    constexpr int W = Tile16<D, FP8>::kVWords;
-    if constexpr (W >= 4) {
-#pragma unroll
-      for (int k = 0; k < W / 4; ++k) {
-        const u32x4 w = *(const u32x4*)(p + 16 * k);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) t.v[i][4 * k + j] = w[j];
-      }
-    } else if constexpr (W == 2) {
-      const u32x2 w = *(const u32x2*)p;
-      t.v[i][0] = w[0];
-      t.v[i][1] = w[1];
-    } else {
-      t.v[i][0] = *(const uint32_t*)p;
-    }
-    if (FP8) t.v_scale[i] = scale_value(__shfl(scale, 32 + key));
-  }
-}
-
 __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale, bool high) {
   const bf16x2 p = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true)
                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
@@ -318,11 +259,139 @@ __device__ __forceinline__ uint32_t widen(uint32_t codes, float scale, bool high
 
 __device__ __forceinline__ bf16x8 as_bf16(u32x4 w) { return __builtin_bit_cast(bf16x8, w); }
 
+__device__ __forceinline__ bf16x8 load_q(const AttendArgs& a, const uint16_t* p, bool there) {
+  u32x4 w = {0, 0, 0, 0};
+  if (there) w = *(const u32x4*)p;
+  return as_bf16(w ^ a.q_sign);
+}
+
+__device__ __forceinline__ void store_bf16x4(uint16_t* p, float x, float y, float z, float w) {
+  const bf16x2 lo = {(__bf16)x, (__bf16)y}, hi = {(__bf16)z, (__bf16)w};
+  *(u32x2*)p = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
 // The running state of one row, on every lane that works for it. `top` is m, or
 // 0 while the row has seen nothing; `sum` a lane's own part.
 struct Soft {
   float m, top, sum;
 };
+
+// A row's result from its sums: minus infinity for a row that saw nothing.
+__device__ __forceinline__ float lse_of(float top, float sum) {
+  return sum == 0.f ? kNone : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+}
+
+// ---- tiles of 16 rows -----------------------------------------------------------------
+// For few rows per request. Every key and value is used by 16 rows at most, so
+// the cache's bytes are what it costs: they go from memory to registers in the
+// layout that the matrix instructions take, with no stop in shared memory. A
+// workgroup's four wavefronts take neighbouring heads of the same keys, whose
+// rows lie side by side (where the number of heads is not a multiple of four or
+// two, keys that follow each other).
+//
+// S^T = K Q^T with mfma 16x16x32: lane l gives key l % 16 and takes row l % 16.
+// Its result holds keys 4 * (l / 16) + i, i < 4, of each half of 32 keys: the
+// eight weights that the lane gives to O^T = V^T P^T, whose sum over keys runs in
+// that order. For V a lane loads D / 16 neighbouring elements of those eight
+// keys and transposes them in registers: product n takes element n of each.
+template <int D, bool FP8>
+struct Tile16 {
+  // keys of a wavefront's step: two steps in flight are what hides the memory's
+  // latency, so short rows come in longer steps
+  static constexpr int kGroups = D * (FP8 ? 1 : 2) < 128 ? 2 : 1;
+  static constexpr int kKeys = 32 * kGroups;
+  static constexpr int kElems = D / 16;                        // of V per lane and key
+  static constexpr int kKWords = FP8 ? D / 16 : D / 8;         // 32-bit words of K per lane and key
+  static constexpr int kVWords = FP8 ? kElems / 4 : kElems / 2;
+  uint32_t k[2 * kGroups][kKWords];
+  uint32_t v[8 * kGroups][kVWords];
+  float k_scale[2 * kGroups], v_scale[8 * kGroups];
+  uint64_t seen;  // which of the keys are to be used
+};
+
+// Where a step's keys are, a lane per key. Pages of whole sixteens of keys: a
+// lane knows the first of its sixteen.
+struct Ids16 {
+  uint32_t page, row;
+  bool in, some;
+};
+
+template <bool EVEN>
+__device__ __forceinline__ Ids16 ids16(const AttendArgs& a, const int32_t* table, int key, const Span& s) {
+  Ids16 x;
+  x.in = key >= s.lo && key < s.hi;
+  const int first = EVEN ? key & ~15 : key;
+  x.some = EVEN ? first + 16 > s.lo && first < s.hi : x.in;
+  const uint32_t at = x.some ? (uint32_t)first : 0u, i = a.b.page.div(at);
+  x.row = at - i * a.b.page.d;
+  x.page = (uint32_t)table[i];
+  return x;
+}
+
+__device__ __forceinline__ int64_t lane_value(int64_t x, uint32_t lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int k = 0; k < N / 4; ++k) {
+      const u32x4 x = *(const u32x4*)(p + 16 * k);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * k + j] = x[j];
+    }
+  } else if constexpr (N == 2) {
+    const u32x2 x = *(const u32x2*)p;
+    w[0] = x[0];
+    w[1] = x[1];
+  } else {
+    w[0] = *(const uint32_t*)p;
+  }
+}
+
+template <int D, bool FP8, bool EVEN>
+__device__ __forceinline__ void load16(const AttendArgs& a, const uint8_t* kp, const uint8_t* vp, uint32_t kv, const Ids16& id,
+                                       Tile16<D, FP8>& t) {
+  typedef Tile16<D, FP8> Tile;
+  constexpr uint32_t kRow = FP8 ? D : 2 * D;  // bytes of a head's row
+  const uint32_t lane = threadIdx.x & 63, c = lane % 16, quad = lane / 16;
+  const bool fine = id.some && id.page < a.c.n_pages;
+  t.seen = __ballot(fine && id.in);
+  // keys that are not to be used are read from page 0
+  const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
+  const uint32_t step = a.n_heads * kRow;  // bytes from a key to the next
+  const int64_t off = page + (fine ? (int64_t)id.row * step : 0) + (int64_t)kv * kRow;
+  uint32_t ks = 127, vs = 127;
+  if (FP8) {
+    const int64_t at = page + a.c.scale_off + kv;
+    ks = scale_held(kp[at]);
+    vs = scale_held(vp[at]);
+  }
+#pragma unroll
+  for (int h = 0; h < 2 * Tile::kGroups; ++h) {
+    const uint8_t* p;
+    if constexpr (EVEN)
+      p = kp + lane_value(off, h * 16) + (c * step + 16 * quad);
+    else
+      p = kp + __shfl(off, h * 16 + c) + 16 * quad;
+#pragma unroll
+    for (int i = 0; i < Tile::kKWords / 4; ++i) load_words<4>(t.k[h] + 4 * i, p + 64 * i);
+    if (FP8) t.k_scale[h] = scale_value(EVEN ? __builtin_amdgcn_readlane(ks, h * 16) : __shfl(ks, h * 16 + c));
+  }
+#pragma unroll
+  for (int i = 0; i < 8 * Tile::kGroups; ++i) {
+    const uint32_t key = quad * 4 + i % 4, half = i / 4 * 16;
+    const uint8_t* p;
+    if constexpr (EVEN)
+      p = vp + lane_value(off, half) + (key * step + kRow / 16 * c);
+    else
+      p = vp + __shfl(off, half + key) + kRow / 16 * c;
+    load_words<Tile::kVWords>(t.v[i], p);
+    if (FP8) t.v_scale[i] = scale_value(EVEN ? __builtin_amdgcn_readlane(vs, half) : __shfl(vs, half + key));
+  }
+}
 
 template <int D, bool FP8>
 struct Rows16 {
@@ -334,10 +403,12 @@ struct Rows16 {
 template <int D, bool FP8>
 __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, int key0, const Place& p, bool edge,
                                         Rows16<D, FP8>& r) {
+  typedef Tile16<D, FP8> Tile;
+  constexpr int N = 8 * Tile::kGroups;
   const uint32_t quad = (threadIdx.x & 63) / 16;
-  float x[8];
+  float x[N];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < 2 * Tile::kGroups; ++h) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {
@@ -354,23 +425,24 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
       acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(w), r.q[k], acc, 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[4 * h + i] = acc[i] * a.scale;
+    for (int i = 0; i < 4; ++i) x[4 * h + i] = acc[i];
   }
-  if (edge || t.seen != ~0u) {  // some row does not see some key
+  if (edge || t.seen != ~0ull) {  // some row does not see some key
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int at = (i / 4) * 16 + quad * 4 + i % 4;
       const bool there = t.seen >> at & 1;
       x[i] = there && key0 + at >= p.lo && key0 + at < p.hi ? x[i] : kNone;
       if (!there) {  // whatever a page holds there, it may be NaN
 #pragma unroll
-        for (int j = 0; j < Tile16<D, FP8>::kVWords; ++j) t.v[i][j] = 0;
+        for (int j = 0; j < Tile::kVWords; ++j) t.v[i][j] = 0;
       }
     }
   }
   float top = x[0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  top *= a.scale;
   if (__any(top > r.s.m + kSlack)) {
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
@@ -383,524 +455,725 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) r.o[i] *= by;
   }
-  bf16x8 w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = exp2_(x[i] - r.s.top);
-    r.s.sum += y;
-    w[i] = (__bf16)y;
-  }
-#pragma unroll
-  for (int n = 0; n < Tile16<D, FP8>::kElems; n += 2) {
-    uint32_t e[8];  // elements n, n + 1 of each key
+  for (int g = 0; g < Tile::kGroups; ++g) {
+    bf16x8 w;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if constexpr (FP8)
-        e[i] = widen(t.v[i][n / 4], t.v_scale[i], n & 2);
-      else
-        e[i] = t.v[i][n / 2];
+      const float y = exp2_(__builtin_fmaf(x[8 * g + i], a.scale, -r.s.top));
+      r.s.sum += y;
+      w[i] = (__bf16)y;
     }
-    u32x4 lo, hi;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x05040100);
-      hi[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x07060302);
+    for (int n = 0; n < Tile::kElems; n += 2) {
+      uint32_t e[8];  // elements n, n + 1 of each key
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (FP8)
+          e[i] = widen(t.v[8 * g + i][n / 4], t.v_scale[8 * g + i], n & 2);
+        else
+          e[i] = t.v[8 * g + i][n / 2];
+      }
+      u32x4 lo, hi;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        lo[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x05040100);
+        hi[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x07060302);
+      }
+      r.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(lo), w, r.o[n], 0, 0, 0);
+      r.o[n + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(hi), w, r.o[n + 1], 0, 0, 0);
     }
-    r.o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(lo), w, r.o[n], 0, 0, 0);
-    r.o[n + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(hi), w, r.o[n + 1], 0, 0, 0);
   }
 }
 
-__device__ __forceinline__ void store_bf16x4(uint16_t* p, float x, float y, float z, float w) {
-  const bf16x2 lo = {(__bf16)x, (__bf16)y}, hi = {(__bf16)z, (__bf16)w};
-  *(u32x2*)p = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-}
+template <int D, int WAVES>
+struct Lds16 {
+  float m[WAVES][16], sum[WAVES][16];
+  float o[WAVES][16][D];
+};
 
-// A row's result from its sums: zeros and minus infinity for a row that saw nothing.
-__device__ __forceinline__ float lse_of(float top, float sum) {
-  return sum == 0.f ? kNone : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
-}
-
-template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void k_attend16(AttendArgs a) {
-  constexpr int M = 16;
-  __shared__ union {
-    PlanLds plan;
-    struct {
-      float m[4][M], sum[4][M];
-      float o[4][M][D];
-    } s;
-  } l;
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, c = lane % 16, quad = lane / 16;
-  Cursor cur;
-  const bool any = plan<kBlock16>(a, l.plan, blockIdx.x, cur);
-  uint32_t worker = blockIdx.x;
-  if (cur.workers == gridDim.x && gridDim.x % 8 == 0) worker = worker % 8 * (gridDim.x / 8) + worker / 8;
-  if (!any) {
-    if (tid == 0) a.share[worker].open = 0;
-    return;
-  }
+// The cursor's blocks of one tile of 16 rows for each of a workgroup's runs of
+// heads, up to the cursor's end or the tile's.
+template <int D, bool FP8, bool EVEN, int WAVES>
+__device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& l, const Cursor& cur, const Request& q, const Span& s,
+                                          uint32_t k0, uint32_t k1) {
+  constexpr int M = 16, E = D / 16;
+  typedef Tile16<D, FP8> Tile;
+  const Kind& kind = a.kind[0];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), c = lane % 16, quad = lane / 16;
+  const uint32_t hs = kind.heads_shift, heads = 1u << hs;
+  const int step = 1 << kind.block_shift;  // keys of a block
   const uint8_t* kp = (const uint8_t*)*a.c.k;
   const uint8_t* vp = (const uint8_t*)*a.c.v;
-  bool first_segment = true;
-  while (cur.at < cur.end) {
+  const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
+  const uint32_t head = (cur.head << hs) + (wave & (heads - 1)), sub = wave >> hs;
+  const uint32_t kv = head / kind.parts;
+  const Place p = place_of(a, kind, q, head, cur.tile, c);
+  Rows16<D, FP8> r;
+  r.s = Soft{kNone, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < E; ++i) r.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  {
+    const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)  // the elements that come with this product's keys
+      r.q[k] = load_q(a, qp + (FP8 ? (k / 2) * 64 + quad * 16 + (k & 1) * 8 : k * 32 + quad * 8), p.there);
+  }
+  // keys below first_hi and from last_lo on are seen by all rows of the tile
+  const int t0 = (int)(cur.tile * kind.tile_rows), t1 = (int)min(cur.tile * kind.tile_rows + kind.tile_rows, q.rows);
+  const int first_hi = a.all ? q.held : min(q.held, q.before + t0 + 1);
+  const int last_lo = a.window ? (int)max((int64_t)0, (int64_t)q.before + t1 - (int64_t)a.window) : 0;
+
+  const int key0 = (int)(s.b0 + k0) * step + (int)sub * Tile::kKeys, last = (int)(s.b0 + k1 - 1) * step + (int)sub * Tile::kKeys;
+  if (s.hi > s.lo) {
+    const int mine = (int)(lane & (Tile::kKeys - 1));
+    auto edge = [&](int key) { return key + Tile::kKeys > first_hi || key < last_lo; };
+    Tile ta, tb;
+    Ids16 id = ids16<EVEN>(a, table, key0 + mine, s);
+    load16<D, FP8, EVEN>(a, kp, vp, kv, id, ta);
+    id = ids16<EVEN>(a, table, min(key0 + step, last) + mine, s);
+    for (int key = key0; key <= last; key += 2 * step) {
+      load16<D, FP8, EVEN>(a, kp, vp, kv, id, tb);
+      id = ids16<EVEN>(a, table, min(key + 2 * step, last) + mine, s);
+      block16<D, FP8>(a, ta, key, p, edge(key), r);
+      if (key + step > last) break;
+      load16<D, FP8, EVEN>(a, kp, vp, kv, id, ta);
+      id = ids16<EVEN>(a, table, min(key + 3 * step, last) + mine, s);
+      block16<D, FP8>(a, tb, key + step, p, edge(key + step), r);
+    }
+  }
+
+  float sum = r.s.sum;
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  const bool whole = k0 == 0 && k1 == s.n;
+  const uint64_t slot = (2 * (uint64_t)cur.worker + (k0 > 0 ? 0 : 1)) * a.slot_rows;
+  // a row's E elements from d0 on, its maximum and its sum, to where they belong
+  auto give = [&](const Place& at, uint32_t m, uint32_t d0, const float* y, float top, float total, bool one) {
+    if (whole) {
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+      uint16_t* op = a.out + (int64_t)at.row * a.o_token + (int64_t)at.head * a.o_head + d0;
+#pragma unroll
+      for (int n = 0; n < E; n += 4) store_bf16x4(op + n, y[n] * inv, y[n + 1] * inv, y[n + 2] * inv, y[n + 3] * inv);
+      if (one && a.lse) a.lse[(uint64_t)at.row * a.n_heads * a.group + at.head] = lse_of(top, total);
+      return;
+    }
+    float* fp = a.part_o + (slot + m) * D + d0;
+#pragma unroll
+    for (int n = 0; n < E; n += 4) *(f32x4*)(fp + n) = f32x4{y[n], y[n + 1], y[n + 2], y[n + 3]};
+    if (one) *(f32x2*)(a.part_ml + (slot + m) * 2) = f32x2{top, total};
+  };
+  if (heads == WAVES) {  // a run of heads for each wavefront
+    if (p.there) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y[E];
+#pragma unroll
+        for (int n = 0; n < E; ++n) y[n] = r.o[n][i];
+        give(p, wave * M + c, (quad * 4 + i) * E, y, r.s.m, sum, i == 0 && quad == 0);
+      }
+    }
+    return;
+  }
+  // the wavefronts' parts of a run
+  __syncthreads();
+  if (quad == 0) {
+    l.m[wave][c] = r.s.m;
+    l.sum[wave][c] = sum;
+  }
+  __syncthreads();
+  float top = kNone;
+  for (uint32_t w = wave & (heads - 1); w < WAVES; w += heads) top = fmaxf(top, l.m[w][c]);
+  const float by = r.s.m == kNone ? 0.f : exp2_(r.s.m - top);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int n = 0; n < E; ++n) l.o[wave][c][(quad * 4 + i) * E + n] = r.o[n][i] * by;
+  __syncthreads();
+  // each thread: E elements of a row
+  for (uint32_t f = tid / 16; f < heads * M; f += 4 * WAVES) {
+    const uint32_t h = f / M, m = f % M, d0 = tid % 16 * E;
+    const Place pm = place_of(a, kind, q, (cur.head << hs) + h, cur.tile, m);
+    if (!pm.there) continue;
+    float row_top = kNone, row_sum = 0.f, y[E];
+    for (uint32_t w = h; w < WAVES; w += heads) row_top = fmaxf(row_top, l.m[w][m]);
+    for (uint32_t w = h; w < WAVES; w += heads) row_sum += l.m[w][m] == kNone ? 0.f : l.sum[w][m] * exp2_(l.m[w][m] - row_top);
+#pragma unroll
+    for (int n = 0; n < E; ++n) y[n] = 0.f;
+    for (uint32_t w = h; w < WAVES; w += heads)
+#pragma unroll
+      for (int n = 0; n < E; ++n) y[n] += l.o[w][m][d0 + n];
+    give(pm, f, d0, y, row_top, row_sum, tid % 16 == 0);
+  }
+}
+
+// Tiles of 16 rows for all requests.
+template <int D, bool FP8, bool EVEN>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a) {
+  __shared__ union {
+    PlanLds plan;
+    Lds16<D, 4> s;
+  } l;
+  Cursor cur;
+  const bool any = plan(a, l.plan, cur);
+  if (!any) {
+    if (threadIdx.x == 0) a.share[cur.worker].parts = 0;
+    return;
+  }
+  for (bool first = true; cur.at < cur.end; first = false) {
     const Request q = request_of(a, cur.r);
-    const Span s = span_of<kBlock16>(a, q.rows, q.held, q.before, cur.tile);
+    const Span s = span_of(a, q, cur.tile);
     const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
-    const uint32_t kv = cur.head / a.parts;
-    const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
-    if (first_segment && tid == 0) {
-      Share& sh = a.share[worker];
-      sh.first = cur.first;
-      sh.end = cur.first + s.n;
-      sh.total = cur.total;
-      sh.workers = cur.workers;
-      sh.r = cur.r;
-      sh.head = cur.head;
-      sh.tile = cur.tile;
-      sh.open = k0 > 0;
-    }
-    first_segment = false;
-
-    const Place p = place_of(a, q, cur.head, cur.tile, c);
-    Rows16<D, FP8> r;
-    r.s = Soft{kNone, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) r.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    {
-      const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
-#pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        // bf16 keys come 64 bytes at a time, codes too: the same elements of q
-        const int at = FP8 ? (k / 2) * 64 + quad * 16 + (k & 1) * 8 : k * 32 + quad * 8;
-        u32x4 w = {0, 0, 0, 0};
-        if (p.there) w = *(const u32x4*)(qp + at);
-        r.q[k] = as_bf16(w);
-      }
-    }
-    // rows of a tile that do not all see the same keys: blocks that some row does not see whole
-    const uint32_t rows_here = min(a.tile_rows, q.rows - cur.tile * a.tile_rows);
-    const int first_hi = a.all ? q.held : min(q.held, q.before + (int)(cur.tile * a.tile_rows) + 1);
-    const int last_lo = a.all || !a.window ? 0 : max(0, (int)min((int64_t)0x7fffffff, (int64_t)q.before + (int)(cur.tile * a.tile_rows + rows_here) - (int64_t)a.window));
-
-    const int key0 = (int)((s.b0 + k0) * kBlock16 + wave * 32);
-    const int last = (int)((s.b0 + k1 - 1) * kBlock16 + wave * 32);
-    if (s.hi > s.lo) {
-      Tile16<D, FP8> ta, tb;
-      Ids16 id = ids16(a, table, key0 + (int)(lane & 31), s);
-      load16<D, FP8>(a, kp, vp, kv, id, ta);
-      id = ids16(a, table, min(key0 + kBlock16, last) + (int)(lane & 31), s);
-      for (int key = key0; key <= last; key += 2 * kBlock16) {
-        load16<D, FP8>(a, kp, vp, kv, id, tb);
-        id = ids16(a, table, min(key + 2 * kBlock16, last) + (int)(lane & 31), s);
-        block16<D, FP8>(a, ta, key, p, key + 32 > first_hi || key < last_lo, r);
-        if (key + kBlock16 > last) break;
-        load16<D, FP8>(a, kp, vp, kv, id, ta);
-        id = ids16(a, table, min(key + 3 * kBlock16, last) + (int)(lane & 31), s);
-        block16<D, FP8>(a, tb, key + kBlock16, p, key + kBlock16 + 32 > first_hi || key + kBlock16 < last_lo, r);
-      }
-    }
-
-    // the four wavefronts' parts
-    float sum = r.s.sum;
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    __syncthreads();
-    if (quad == 0) {
-      l.s.m[wave][c] = r.s.m;
-      l.s.sum[wave][c] = sum;
-    }
-    __syncthreads();
-    float top = kNone;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, l.s.m[w][c]);
-    const float by = r.s.m == kNone ? 0.f : exp2_(r.s.m - top);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int n = 0; n < D / 16; ++n) l.s.o[wave][c][(quad * 4 + i) * (D / 16) + n] = r.o[n][i] * by;
-    __syncthreads();
-    // each thread: D / 16 elements of one row
-    const uint32_t m = tid / 16, d0 = tid % 16 * (D / 16);
-    float row_top = kNone, row_sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) row_top = fmaxf(row_top, l.s.m[w][m]);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) row_sum += l.s.m[w][m] == kNone ? 0.f : l.s.sum[w][m] * exp2_(l.s.m[w][m] - row_top);
-    const Place pm = place_of(a, q, cur.head, cur.tile, m);
-    const bool whole = k0 == 0 && k1 == s.n;
-    if (pm.there) {
-      const float inv = row_sum == 0.f ? 0.f : 1.f / row_sum;
-      const uint64_t slot = 2 * (uint64_t)worker + (k0 > 0 ? 0 : 1);
-      uint16_t* op = a.out + (int64_t)pm.row * a.o_token + (int64_t)pm.head * a.o_head + d0;
-      float* fp = a.part_o + (slot * M + m) * D + d0;
-#pragma unroll
-      for (int n = 0; n < D / 16; n += 4) {
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) y += *(const f32x4*)&l.s.o[w][m][d0 + n];
-        if (whole)
-          store_bf16x4(op + n, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-        else
-          *(f32x4*)(fp + n) = y;
-      }
-      if (tid % 16 == 0) {
-        if (!whole) {
-          a.part_ml[(slot * M + m) * 2] = row_top;
-          a.part_ml[(slot * M + m) * 2 + 1] = row_sum;
-        } else if (a.lse) {
-          a.lse[(uint64_t)pm.row * a.n_heads * a.group + pm.head] = lse_of(row_top, row_sum);
-        }
-      }
-    }
+    if (first && threadIdx.x == 0) note_share(a, cur, q, s);
+    segment16<D, FP8, EVEN, 4>(a, l.s, cur, q, s, k0, k1);
     cur.at = cur.first + k1;
     if (k1 == s.n) {
       cur.first += s.n;
-      if (cur.at < cur.end) next_tile(a, cur);
+      if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
 }
 
-// ---- tiles of 128 rows --------------------------------------------------------------
-// For prompts. A block of 64 keys and values is widened to bf16 once, into shared
-// memory, and used by the 32 rows of each of four wavefronts; the next block's
-// bytes are on their way meanwhile.
+// ---- tiles of 32 rows for each wavefront ---------------------------------------------------
+// For prompts. A block of keys and values is widened to bf16 once, into shared
+// memory, and used by the 32 rows of each wavefront.
 //
 // S^T = K Q^T with mfma 32x32x16: lane l takes row l % 32, and its result holds
 // keys 8 * (i / 4) + 4 * (l / 32) + i % 4. Registers 8a .. 8a + 7 are what the
 // lane gives to step a of O^T = V^T P^T, whose keys run in that order: V comes
 // from shared memory through transposing reads of four keys each.
-constexpr int kBlock128 = 64;
-
+//
+// With eight wavefronts two share a SIMD. They work in opposite phases, with a
+// barrier after each: while one wavefront's products (P V of this block, Q K of the
+// next) use the matrix unit, the other's exponentials use the vector unit.
 template <int D>
-struct Lds128 {
-  uint16_t k[kBlock128 * D], v[kBlock128 * D];
-  int64_t off[2][kBlock128];       // byte offsets of the keys' rows
-  uint32_t scale[2][kBlock128];    // scale bytes: K's, and V's in bits 8 to 15; 0: not to be used
-  uint64_t seen[2];                // keys that are to be used
+struct Lds32 {
+  static constexpr int KT = D == 256 ? 32 : 64;  // keys of a block
+  alignas(1024) uint16_t k[2][KT * D];
+  uint16_t v[2][KT * D];
+  int64_t off[4][KT];     // byte offsets of the keys' rows
+  uint32_t scale[4][KT];  // scale bytes: K's, and V's in bits 8 to 15; 0: not to be used
+  uint64_t seen[4];       // keys that are to be used
 };
 
-// Where 8 neighbouring elements, chunk c of key r, are kept: such that lanes
-// that read together use all banks.
+typedef __attribute__((address_space(3))) const char* LdsAddress;
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsAddress)p; }
+
+// Where an element is kept: such that lanes that read or write together use all
+// banks. K: 8 neighbouring elements, chunk c of key r.
+template <int D>
+__device__ __forceinline__ constexpr uint32_t k_swap(uint32_t r) {
+  return D == 64 ? r >> 1 & 7 : r & 15;
+}
 template <int D>
 __device__ __forceinline__ uint32_t k_at(uint32_t r, uint32_t c) {
-  return r * D + (c ^ (r & 7)) * 8;
+  return r * D + (c ^ k_swap<D>(r)) * 8;
+}
+// V: elem a multiple of 4.
+template <int D>
+__device__ __forceinline__ uint32_t v_swap(uint32_t r) {
+  return (D == 64 ? (r >> 1 & 1) : (r & 3)) * 32 + (r & 1) * 8;
 }
 template <int D>
-__device__ __forceinline__ uint32_t v_at(uint32_t r, uint32_t elem) {  // elem: a multiple of 4
-  const uint32_t sw = D == 64 ? (r >> 1 & 1) : (r & 3);
-  return r * D + (elem ^ (sw * 32));
+__device__ __forceinline__ uint32_t v_at(uint32_t r, uint32_t elem) {
+  return r * D + (elem ^ v_swap<D>(r));
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void k_attend128(AttendArgs a) {
-  constexpr int M = 128, KT = kBlock128;
-  constexpr int kRow = FP8 ? D : 2 * D;
-  constexpr int kLoads = KT * kRow / 16 / kThreads;  // 16-byte pieces of K (and of V) per thread
-  constexpr int kPieces = kRow / 16;                 // pieces of a key
-  __shared__ union {
-    PlanLds plan;
-    Lds128<D> s;
-  } l;
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64, c = lane % 32, half = lane / 32;
-  Cursor cur;
-  const bool any = plan<KT>(a, l.plan, blockIdx.x, cur);
-  uint32_t worker = blockIdx.x;
-  if (cur.workers == gridDim.x && gridDim.x % 8 == 0) worker = worker % 8 * (gridDim.x / 8) + worker / 8;
-  if (!any) {
-    if (tid == 0) a.share[worker].open = 0;
-    return;
-  }
+template <int D, bool FP8, int WAVES>
+__device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, const Cursor& cur, const Request& q, const Span& s,
+                                          uint32_t k0, uint32_t k1) {
+  constexpr int KT = Lds32<D>::KT, NB = KT / 32, kThreads = 64 * WAVES;
+  constexpr int kRow = FP8 ? D : 2 * D;                             // bytes of a head's row
+  constexpr int kPieces = kRow / 16;                                // 16-byte pieces of a key
+  constexpr int kLoads = (KT * kPieces + kThreads - 1) / kThreads;  // of K (and of V) per thread
+  constexpr bool kSpare = KT * kPieces % kThreads != 0;             // some threads have none
+  constexpr uint32_t kBatch = 4, kDs = D == 64 ? 2 : 4;             // products whose operands are read at a time
+  constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : 0xffffffffull;
+  const Kind& kind = a.kind[1];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, c = lane % 32, half = lane / 32;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const uint8_t* kp = (const uint8_t*)*a.c.k;
   const uint8_t* vp = (const uint8_t*)*a.c.v;
-  bool first_segment = true;
-  while (cur.at < cur.end) {
-    const Request q = request_of(a, cur.r);
-    const Span s = span_of<KT>(a, q.rows, q.held, q.before, cur.tile);
-    const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
-    const uint32_t kv = cur.head / a.parts;
-    const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
-    if (first_segment && tid == 0) {
-      Share& sh = a.share[worker];
-      sh.first = cur.first;
-      sh.end = cur.first + s.n;
-      sh.total = cur.total;
-      sh.workers = cur.workers;
-      sh.r = cur.r;
-      sh.head = cur.head;
-      sh.tile = cur.tile;
-      sh.open = k0 > 0;
-    }
-    first_segment = false;
+  const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
+  const uint32_t kv = cur.head / kind.parts;
 
-    const uint32_t m = wave * 32 + c;
-    const Place p = place_of(a, q, cur.head, cur.tile, m);
-    bf16x8 qf[D / 16];
-    {
-      const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
+  const uint32_t m = wave * 32 + c;
+  const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
+  bf16x8 qf[D / 16];
+  {
+    const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        u32x4 w = {0, 0, 0, 0};
-        if (p.there) w = *(const u32x4*)(qp + k * 16 + half * 8);
-        qf[k] = as_bf16(w);
-      }
+    for (int k = 0; k < D / 16; ++k) qf[k] = load_q(a, qp + k * 16 + half * 8, p.there);
+  }
+  // keys that some row of this wavefront sees, and keys that all of them see
+  int wave_lo, wave_hi, all_lo, all_hi;
+  {
+    int lo = p.there ? p.lo : 0x7fffffff, hi = p.there ? p.hi : 0, lo2 = p.there ? p.lo : 0, hi2 = p.there ? p.hi : 0x7fffffff;
+    for (uint32_t k = 1; k < 32; k *= 2) {
+      lo = min(lo, __shfl_xor(lo, k));
+      hi = max(hi, __shfl_xor(hi, k));
+      lo2 = max(lo2, __shfl_xor(lo2, k));
+      hi2 = min(hi2, __shfl_xor(hi2, k));
     }
-    // keys that some row of this wavefront sees, and keys that all of them see
-    int wave_lo, wave_hi, all_lo, all_hi;
-    {
-      int lo = p.there ? p.lo : 0x7fffffff, hi = p.there ? p.hi : 0, lo2 = p.there ? p.lo : 0, hi2 = p.there ? p.hi : 0x7fffffff;
-      for (uint32_t k = 1; k < 32; k *= 2) {
-        lo = min(lo, __shfl_xor(lo, k));
-        hi = max(hi, __shfl_xor(hi, k));
-        lo2 = max(lo2, __shfl_xor(lo2, k));
-        hi2 = min(hi2, __shfl_xor(hi2, k));
-      }
-      wave_lo = __builtin_amdgcn_readfirstlane(lo);
-      wave_hi = __builtin_amdgcn_readfirstlane(hi);
-      all_lo = __builtin_amdgcn_readfirstlane(lo2);
-      all_hi = __builtin_amdgcn_readfirstlane(hi2);
-    }
-    f32x16 o[D / 32];
+    wave_lo = __builtin_amdgcn_readfirstlane(lo);
+    wave_hi = __builtin_amdgcn_readfirstlane(hi);
+    all_lo = __builtin_amdgcn_readfirstlane(lo2);
+    all_hi = __builtin_amdgcn_readfirstlane(hi2);
+  }
+  f32x16 o[D / 32];
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+  for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    Soft st = {kNone, 0.f, 0.f};
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  Soft st = {kNone, 0.f, 0.f};
 
-    const int block0 = (int)(s.b0 + k0) * KT, block_last = (int)(s.b0 + k1 - 1) * KT;
-    u32x4 kr[kLoads], vr[kLoads];
-    // wavefront 0: where the keys of a block are
-    auto find = [&](int key0, Ids16& id) {
-      if (wave == 0) id = ids16(a, table, key0 + (int)lane, s);
-    };
-    auto scales = [&](const Ids16& id, uint32_t& ks, uint32_t& vs) {
-      if (!FP8 || wave != 0) return;
-      const int64_t at = (id.in && id.page < a.c.n_pages ? (int64_t)id.page * a.c.stride : 0) + a.c.scale_off + kv;
-      ks = kp[at];
-      vs = vp[at];
-    };
-    auto note = [&](const Ids16& id, uint32_t ks, uint32_t vs, uint32_t slot) {
-      if (wave != 0) return;
-      const bool fine = id.in && id.page < a.c.n_pages;
-      const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
-      uint32_t sc = 0x7f7f;
-      if (FP8) sc = scale_held(ks) | scale_held(vs) << 8;
-      l.s.off[slot][lane] = page + (fine ? (int64_t)id.row * a.n_heads * kRow : 0) + (int64_t)kv * kRow;
-      l.s.scale[slot][lane] = fine ? sc : 0;
-      const uint64_t seen = __ballot(fine);
-      if (lane == 0) l.s.seen[slot] = seen;
-    };
-    auto fetch = [&](uint32_t slot) {
+  const int blocks = (int)(k1 - k0), block0 = (int)(s.b0 + k0) * KT, block_last = (int)(s.b0 + k1 - 1) * KT;
+  u32x4 kr[kLoads], vr[kLoads];
+  // wavefront 0: where the keys of block n are
+  auto find = [&](int n, Ids16& id) {
+    if (wave == 0) id = ids16<false>(a, table, min(block0 + n * KT, block_last) + (int)(lane % KT), s);
+  };
+  auto scales = [&](const Ids16& id, uint32_t& ks, uint32_t& vs) {
+    if (!FP8 || wave != 0) return;
+    const int64_t at = (id.in && id.page < a.c.n_pages ? (int64_t)id.page * a.c.stride : 0) + a.c.scale_off + kv;
+    ks = kp[at];
+    vs = vp[at];
+  };
+  auto note = [&](const Ids16& id, uint32_t ks, uint32_t vs, uint32_t n) {
+    if (wave != 0) return;
+    const uint32_t slot = n & 3;
+    const bool fine = id.in && id.page < a.c.n_pages;
+    const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
+    uint32_t sc = 0x7f7f;
+    if (FP8) sc = scale_held(ks) | scale_held(vs) << 8;
+    const uint64_t seen = __ballot(fine);
+    if (KT == 64 || lane < KT) {
+      l.off[slot][lane] = page + (fine ? (int64_t)id.row * a.n_heads * kRow : 0) + (int64_t)kv * kRow;
+      l.scale[slot][lane] = fine ? sc : 0;
+    }
+    if (lane == 0) l.seen[slot] = KT == 64 ? seen : seen & kAllSeen;
+  };
+  // a thread's pieces of block n, on their way from memory, and into shared memory
+  auto fetch = [&](u32x4* to, const uint8_t* from, uint32_t n) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
-        const int64_t off = l.s.off[slot][row] + piece * 16;
-        kr[i] = *(const u32x4*)(kp + off);
-        vr[i] = *(const u32x4*)(vp + off);
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
+      if (kSpare && row >= KT) continue;
+      to[i] = *(const u32x4*)(from + l.off[n & 3][row] + piece * 16);
+    }
+  };
+  auto keep_k = [&](uint32_t n) {
+    uint16_t* to = l.k[n & 1];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
+      if (kSpare && row >= KT) continue;
+      if constexpr (FP8) {
+        const float by = scale_value(l.scale[n & 3][row] & 0xff);
+        u32x4 w[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j / 2][j % 2 * 2] = widen(kr[i][j], by, false);
+          w[j / 2][j % 2 * 2 + 1] = widen(kr[i][j], by, true);
+        }
+        *(u32x4*)(to + k_at<D>(row, 2 * piece)) = w[0];
+        *(u32x4*)(to + k_at<D>(row, 2 * piece + 1)) = w[1];
+      } else {
+        *(u32x4*)(to + k_at<D>(row, piece)) = kr[i];
+      }
+    }
+  };
+  auto keep_v = [&](uint32_t n) {
+    uint16_t* to = l.v[n & 1];
+    const bool every = l.seen[n & 3] == kAllSeen;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
+      if (kSpare && row >= KT) continue;
+      const uint32_t sc = l.scale[n & 3][row];
+      u32x4 x = vr[i];
+      if (!every && !sc) x = u32x4{0, 0, 0, 0};  // whatever a page holds there, it may be NaN
+      if constexpr (FP8) {
+        const float by = scale_value(sc >> 8);
+        u32x4 w[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j / 2][j % 2 * 2] = widen(x[j], by, false);
+          w[j / 2][j % 2 * 2 + 1] = widen(x[j], by, true);
+        }
+        *(u32x4*)(to + v_at<D>(row, 16 * piece)) = w[0];
+        *(u32x4*)(to + v_at<D>(row, 16 * piece + 8)) = w[1];
+      } else {
+        *(u32x4*)(to + v_at<D>(row, 8 * piece)) = x;
+      }
+    }
+  };
+
+  // Where this lane finds its part of a product's K and V, in bytes of shared
+  // memory. The product's number goes in by an exclusive or, at the read itself:
+  // one register each, not one for each product.
+  const uint32_t k_lane = lds_of(l.k[0]) + c * D * 2 + (half ^ (k_swap<D>(c) & 1)) * 16 + k_swap<D>(c) / 2 * 32;
+  const uint32_t v_row = half * 4 + lane % 16 / 4;
+  const uint32_t v_lane = lds_of(l.v[0]) + v_row * D * 2 + ((lane / 16 % 2 * 16 + lane % 4 * 4) ^ v_swap<D>(v_row)) * 2;
+  f32x16 x[NB];  // a block's scores
+  bf16x8 w[2 * NB];  // and weights
+
+  auto used = [&](int n) { return block0 + n * KT < wave_hi && block0 + n * KT + KT > wave_lo; };
+  // x = K Q^T of block n, the operands read a batch ahead
+  auto scores = [&](uint32_t n) {
+    const uint32_t from = k_lane + (n & 1) * KT * D * 2;
+    u32x4 kf[2][kBatch];
+    auto read = [&](uint32_t i) {
+#pragma unroll
+      for (uint32_t j = 0; j < kBatch; ++j) {
+        const uint32_t at = i * kBatch + j, b = at / (D / 16), k = at % (D / 16);
+        kf[i & 1][j] = *(__attribute__((address_space(3))) const u32x4*)((LdsAddress)(uintptr_t)(from ^ k * 32) + b * 32 * D * 2);
       }
     };
-    auto keep = [&](uint32_t slot) {
+    read(0);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
-        const uint32_t sc = l.s.scale[slot][row];
-        if constexpr (FP8) {
-          const float ks = scale_value(sc & 0xff), vs = scale_value(sc >> 8);
-          u32x4 w[4];
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            w[j / 2][j % 2 * 2] = widen(kr[i][j], ks, false);
-            w[j / 2][j % 2 * 2 + 1] = widen(kr[i][j], ks, true);
-            w[2 + j / 2][j % 2 * 2] = sc ? widen(vr[i][j], vs, false) : 0;
-            w[2 + j / 2][j % 2 * 2 + 1] = sc ? widen(vr[i][j], vs, true) : 0;
-          }
-          *(u32x4*)(l.s.k + k_at<D>(row, 2 * piece)) = w[0];
-          *(u32x4*)(l.s.k + k_at<D>(row, 2 * piece + 1)) = w[1];
-          *(u32x4*)(l.s.v + v_at<D>(row, 16 * piece)) = w[2];
-          *(u32x4*)(l.s.v + v_at<D>(row, 16 * piece + 8)) = w[3];
-        } else {
-          *(u32x4*)(l.s.k + k_at<D>(row, piece)) = kr[i];
-          *(u32x4*)(l.s.v + v_at<D>(row, 8 * piece)) = sc ? vr[i] : u32x4{0, 0, 0, 0};
+      for (int j = 0; j < 16; ++j) x[b][j] = 0.f;
+#pragma unroll
+    for (uint32_t i = 0; i < NB * D / 16 / kBatch; ++i) {
+      if (i + 1 < NB * D / 16 / kBatch) read(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (uint32_t j = 0; j < kBatch; ++j) {
+        const uint32_t at = i * kBatch + j, b = at / (D / 16), k = at % (D / 16);
+        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(kf[i & 1][j]), qf[k], x[b], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // w = the weights of block n
+  auto weigh = [&](uint32_t n) {
+    const int key0 = block0 + (int)n * KT;
+    const uint64_t seen = l.seen[n & 3];
+    if (seen != kAllSeen || key0 < all_lo || key0 + KT > all_hi) {  // some row does not see some key
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const uint32_t bits = (uint32_t)(seen >> (32 * b)) >> (4 * half);
+        const int first = key0 + 32 * b + 4 * (int)half;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int at = 8 * (j / 4) + j % 4;
+          const bool there = (bits >> at & 1) && first + at >= p.lo && first + at < p.hi;
+          x[b][j] = there ? x[b][j] : kNone;
         }
       }
+    }
+    float top = x[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, x[b][j]);
+    top *= a.scale;
+    if (__any(top > st.m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mm = fmaxf(st.m, top);
+      const float now = mm == kNone ? 0.f : mm;
+      const float by = st.m == kNone ? 0.f : exp2_(st.top - now);
+      st.m = mm;
+      st.top = now;
+      st.sum *= by;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] *= by;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const float y = exp2_(__builtin_fmaf(x[b][j], a.scale, -st.top));
+        st.sum += y;
+        w[2 * b + j / 8][j % 8] = (__bf16)y;
+      }
+  };
+  // o += V^T w of block n, the operands read a batch ahead
+  auto values = [&](uint32_t n) {
+    const uint32_t from = v_lane + (n & 1) * KT * D * 2;
+    constexpr uint32_t kSteps = 2 * NB * (D / 32) / kDs;
+    u32x2 vf[2][2 * kDs];
+    auto read = [&](uint32_t i) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* Lds4;
+#pragma unroll
+      for (uint32_t j = 0; j < kDs; ++j) {
+        const uint32_t t = i / (D / 32 / kDs), d = i % (D / 32 / kDs) * kDs + j;
+        const LdsAddress v = (LdsAddress)(uintptr_t)(from ^ d * 64) + t * 16 * D * 2;
+        vf[i & 1][2 * j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)v));
+        vf[i & 1][2 * j + 1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(v + 8 * D * 2)));
+      }
     };
+    read(0);
+#pragma unroll
+    for (uint32_t i = 0; i < kSteps; ++i) {
+      if (i + 1 < kSteps) read(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (uint32_t j = 0; j < kDs; ++j) {
+        const uint32_t t = i / (D / 32 / kDs), d = i % (D / 32 / kDs) * kDs + j;
+        const u32x2 lo = vf[i & 1][2 * j], hi = vf[i & 1][2 * j + 1];
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]}), w[t], o[d], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
 
-    const bool some = s.hi > s.lo;
-    if (some) {
-      Ids16 id, later;
-      uint32_t ks = 0, vs = 0;
-      __syncthreads();
-      find(block0, id);
+  if (s.hi > s.lo) {
+    // Block n is noted in slot n % 4 and kept in buffers n % 2. Past the last
+    // block the last one is read again.
+    Ids16 id, later;
+    uint32_t ks = 0, vs = 0;
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      find(n, id);
       scales(id, ks, vs);
-      note(id, ks, vs, 0);
-      find(min(block0 + KT, block_last), id);
-      scales(id, ks, vs);
-      note(id, ks, vs, 1);
-      find(min(block0 + 2 * KT, block_last), id);
+      note(id, ks, vs, n);
+    }
+    find(3, id);
+    __syncthreads();
+    fetch(kr, kp, 0);
+    keep_k(0);
+    if constexpr (WAVES == 8) {
+      // Wavefronts 0 to 3 are a phase ahead. A step of theirs keeps and fetches
+      // K of the next block and V of this one; the others', a phase later, those
+      // of the block after, so that all of it is there a phase before its use.
+      const uint32_t behind = wave / 4;
+      fetch(kr, kp, 1);
+      fetch(vr, vp, 0);
       __syncthreads();
-      fetch(0);
-      uint32_t slot = 0;
-      for (int key0 = block0; key0 <= block_last; key0 += KT, slot ^= 1) {
-        keep(slot);
-        const uint64_t seen = l.s.seen[slot];
+      if (used(0)) scores(0);
+      auto bring = [&](uint32_t n) {  // K of block n + 1 and V of block n into shared memory
+        keep_k(n + 1);
+        keep_v(n);
+        fetch(kr, kp, n + 2);
+        fetch(vr, vp, n + 1);
+      };
+      if (behind) {
+        bring(0);
         __syncthreads();
-        fetch(slot ^ 1);
+      }
+      for (int n = 0; n < blocks; ++n) {
         scales(id, ks, vs);
-        find(min(key0 + 3 * KT, block_last), later);
-        if (key0 < wave_hi && key0 + KT > wave_lo) {
-          float x[2][16];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            f32x16 acc;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const u32x4 w = *(const u32x4*)(l.s.k + k_at<D>(b * 32 + c, 2 * k + half));
-              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(w), qf[k], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x[b][j] = acc[j] * a.scale;
-          }
-          if (seen != ~0ull || key0 < all_lo || key0 + KT > all_hi) {
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int at = b * 32 + 8 * (j / 4) + 4 * half + j % 4;
-                const bool there = (seen >> at & 1) && key0 + at >= p.lo && key0 + at < p.hi;
-                x[b][j] = there ? x[b][j] : kNone;
-              }
-          }
-          float top = x[0][0];
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, x[b][j]);
-          if (__any(top > st.m + kSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float mm = fmaxf(st.m, top);
-            const float now = mm == kNone ? 0.f : mm;
-            const float by = st.m == kNone ? 0.f : exp2_(st.top - now);
-            st.m = mm;
-            st.top = now;
-            st.sum *= by;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) o[i] *= by;
-          }
-          bf16x8 w[4];
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float y = exp2_(x[b][j] - st.top);
-              st.sum += y;
-              w[2 * b + j / 8][j % 8] = (__bf16)y;
-            }
-#pragma unroll
-          for (int st4 = 0; st4 < 4; ++st4) {
-            const uint32_t i = lane % 16, key = st4 * 16 + half * 4 + i / 4;
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d) {
-              const uint32_t elem = d * 32 + (lane / 16 % 2) * 16 + i % 4 * 4;
-              typedef short s16x4 __attribute__((ext_vector_type(4)));
-              typedef __attribute__((address_space(3))) s16x4* Lds4;
-              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(l.s.v + v_at<D>(key, elem)));
-              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(l.s.v + v_at<D>(key + 8, elem)));
-              const u32x2 lw = __builtin_bit_cast(u32x2, lo), hw = __builtin_bit_cast(u32x2, hi);
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(u32x4{lw[0], lw[1], hw[0], hw[1]}), w[st4], o[d], 0, 0, 0);
-            }
-          }
+        find(n + 4, later);
+        if (used(n)) weigh(n);
+        bring(n + behind);
+        note(id, ks, vs, n + 3);
+        id = later;
+        __syncthreads();
+        if (used(n)) values(n);
+        if (n + 1 < blocks && used(n + 1)) scores(n + 1);
+        __syncthreads();
+      }
+      if (!behind) __syncthreads();
+    } else {
+      // A step uses one block, keeps the next and fetches the one after.
+      fetch(vr, vp, 0);
+      keep_v(0);
+      fetch(kr, kp, 1);
+      fetch(vr, vp, 1);
+      __syncthreads();
+      for (int n = 0; n < blocks; ++n) {
+        scales(id, ks, vs);
+        find(n + 4, later);
+        const bool use = used(n);
+        if (use) scores(n);
+        keep_k(n + 1);
+        keep_v(n + 1);
+        fetch(kr, kp, n + 2);
+        fetch(vr, vp, n + 2);
+        if (use) {
+          weigh(n);
+          values(n);
         }
-        note(id, ks, vs, slot);
+        note(id, ks, vs, n + 3);
         id = later;
         __syncthreads();
       }
     }
+  }
 
-    float sum = st.sum + __shfl_xor(st.sum, 32);
-    const bool whole = k0 == 0 && k1 == s.n;
-    if (p.there) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      const uint64_t slot = 2 * (uint64_t)worker + (k0 > 0 ? 0 : 1);
-      uint16_t* op = a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head;
-      float* fp = a.part_o + (slot * M + m) * D;
+  const float sum = st.sum + __shfl_xor(st.sum, 32);
+  const bool whole = k0 == 0 && k1 == s.n;
+  if (p.there) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const uint64_t slot = (2 * (uint64_t)cur.worker + (k0 > 0 ? 0 : 1)) * a.slot_rows;
+    uint16_t* op = a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head;
+    float* fp = a.part_o + (slot + m) * D;
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          const uint32_t at = d * 32 + 2 * j + 4 * half;
-          if (whole)
-            store_bf16x4(op + at, o[d][j] * inv, o[d][j + 1] * inv, o[d][j + 2] * inv, o[d][j + 3] * inv);
-          else
-            *(f32x4*)(fp + at) = f32x4{o[d][j], o[d][j + 1], o[d][j + 2], o[d][j + 3]};
-        }
-      if (half == 0) {
-        if (!whole) {
-          a.part_ml[(slot * M + m) * 2] = st.m;
-          a.part_ml[(slot * M + m) * 2 + 1] = sum;
-        } else if (a.lse) {
-          a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(st.top, sum);
-        }
+      for (int j = 0; j < 16; j += 4) {
+        const uint32_t at = d * 32 + 2 * j + 4 * half;
+        if (whole)
+          store_bf16x4(op + at, o[d][j] * inv, o[d][j + 1] * inv, o[d][j + 2] * inv, o[d][j + 3] * inv);
+        else
+          *(f32x4*)(fp + at) = f32x4{o[d][j], o[d][j + 1], o[d][j + 2], o[d][j + 3]};
       }
+    if (half == 0) {
+      if (!whole)
+        *(f32x2*)(a.part_ml + (slot + m) * 2) = f32x2{st.m, sum};
+      else if (a.lse)
+        a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(st.top, sum);
     }
+  }
+}
+
+// Tiles of 32 rows for each wavefront, and of 16 for requests of few rows.
+template <int D, bool FP8, bool EVEN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend32(AttendArgs a) {
+  __shared__ union {
+    PlanLds plan;
+    Lds16<D, WAVES> few;
+    Lds32<D> many;
+  } l;
+  Cursor cur;
+  const bool any = plan(a, l.plan, cur);
+  if (!any) {
+    if (threadIdx.x == 0) a.share[cur.worker].parts = 0;
+    return;
+  }
+  for (bool first = true; cur.at < cur.end; first = false) {
+    const Request q = request_of(a, cur.r);
+    const Span s = span_of(a, q, cur.tile);
+    const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
+    if (first && threadIdx.x == 0) note_share(a, cur, q, s);
+    if (q.kind)
+      segment32<D, FP8, WAVES>(a, l.many, cur, q, s, k0, k1);
+    else
+      segment16<D, FP8, EVEN, WAVES>(a, l.few, cur, q, s, k0, k1);
     cur.at = cur.first + k1;
     if (k1 == s.n) {
       cur.first += s.n;
-      if (cur.at < cur.end) next_tile(a, cur);
+      if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
 }
 
 // ---- joining ---------------------------------------------------------------------------
-// A tile that several workers share: the workgroup of the second of them (the
-// first that goes on with it) adds up their parts, in the workers' order.
-template <int M, int D>
-__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a) {
-  const uint32_t worker = blockIdx.x + 1;
+// A tile that several workers share: the workgroups of the second of them add up
+// their parts. A run of D / 4 threads takes a row; where there are fewer rows than
+// runs, several take every so manieth of a row's parts. The order of the sums
+// follows from the sizes alone.
+template <int D>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+  constexpr uint32_t kLanes = D / 4, kRuns = 256 / kLanes;
+  constexpr int kAhead = 4;
+  __shared__ struct {
+    float top[kRuns], sum[kRuns];
+    f32x4 y[kRuns][kLanes];
+  } l;
+  const uint32_t split = a.slot_rows / kRuns;  // workgroups of a worker
+  const uint32_t worker = blockIdx.x / split + 1, row0 = blockIdx.x % split * kRuns;
   const Share sh = a.share[worker];
-  if (!sh.open) return;
-  auto start = [&](uint64_t w) { return sh.total * w / sh.workers; };
-  if (start(worker - 1) > sh.first) return;  // the worker before goes on with it as well
-  uint32_t last = worker;
-  while (start(last + 1) < sh.end) ++last;
-  const Request q = request_of(a, sh.r);
-  constexpr int kLanes = D / 4;  // of a row
-  for (uint32_t m = threadIdx.x / kLanes; m < M; m += kThreads / kLanes) {
-    const Place p = place_of(a, q, sh.head, sh.tile, m);
-    if (!p.there) continue;
-    const uint32_t d = threadIdx.x % kLanes * 4;
-    float top = kNone;
-    for (uint32_t w = worker - 1; w <= last; ++w) {
-      const uint64_t slot = 2 * (uint64_t)w + (w < worker ? 1 : 0);
-      top = fmaxf(top, a.part_ml[(slot * M + m) * 2]);
+  if (!sh.parts) return;
+  const Kind& kind = a.kind[sh.kind];
+  if (row0 >= kind.rows << kind.heads_shift) return;
+  Request q = {};
+  q.row0 = sh.row0;
+  q.rows = sh.rows;
+  // rows [row0, row0 + kRuns) of the part: of one run of heads, m0 its first
+  const uint32_t head = (sh.head << kind.heads_shift) + row0 / kind.rows, m0 = row0 % kind.rows;
+  const uint32_t tokens = min(kind.tile_rows, sh.rows - sh.tile * kind.tile_rows), rows = tokens * kind.part_heads;
+  if (m0 >= rows) return;
+  uint32_t slices = kRuns;  // of a row's parts
+  while (slices > 1 && (rows - m0) * slices > kRuns) slices /= 2;
+  const uint32_t run = threadIdx.x / kLanes, d = threadIdx.x % kLanes, i = run / slices, slice = run % slices, m = m0 + i;
+  const Place p = place_of(a, kind, q, head, sh.tile, min(m, kind.rows - 1));
+  float top = kNone, sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  const bool there = p.there && m < kind.rows;
+  if (there) {
+    for (uint32_t w0 = slice; w0 < sh.parts; w0 += slices * kAhead) {
+      f32x2 ml[kAhead];
+      f32x4 o[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t w = min(w0 + k * slices, sh.parts - 1);
+        const uint64_t at = (2 * (uint64_t)(worker - 1 + w) + (w == 0 ? 1 : 0)) * a.slot_rows + row0 + i;
+        ml[k] = *(const f32x2*)(a.part_ml + at * 2);
+        o[k] = *(const f32x4*)(a.part_o + at * D + 4 * d);
+        if (w0 + k * slices >= sh.parts) ml[k][0] = kNone;
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (ml[k][0] == kNone) continue;
+        const float now = fmaxf(top, ml[k][0]);
+        const float old = top == kNone ? 0.f : exp2_(top - now), by = exp2_(ml[k][0] - now);
+        sum = sum * old + ml[k][1] * by;
+        y = y * old + o[k] * by;
+        top = now;
+      }
     }
-    float sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t w = worker - 1; w <= last; ++w) {
-      const uint64_t slot = 2 * (uint64_t)w + (w < worker ? 1 : 0);
-      const float pm = a.part_ml[(slot * M + m) * 2];
-      const float by = pm == kNone ? 0.f : exp2_(pm - top);
-      sum += a.part_ml[(slot * M + m) * 2 + 1] * by;
-      y += *(const f32x4*)(a.part_o + (slot * M + m) * D + d) * by;
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    store_bf16x4(a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head + d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-    if (a.lse && d == 0) a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(top, sum);
   }
+  if (slices > 1) {
+    if (d == 0) {
+      l.top[run] = top;
+      l.sum[run] = sum;
+    }
+    l.y[run][d] = y;
+    __syncthreads();
+    if (slice) return;
+    const float mine = top;
+    for (uint32_t k = 1; k < slices; ++k) top = fmaxf(top, l.top[run + k]);
+    const float by0 = mine == kNone ? 0.f : exp2_(mine - top);
+    sum *= by0;
+    y *= by0;
+    for (uint32_t k = 1; k < slices; ++k) {
+      const float by = l.top[run + k] == kNone ? 0.f : exp2_(l.top[run + k] - top);
+      sum += l.sum[run + k] * by;
+      y += l.y[run + k][d] * by;
+    }
+  }
+  if (!there) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  store_bf16x4(a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head + 4 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+  if (a.lse && d == 0) a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(top, sum);
 }
 
 // ---- launching ----------------------------------------------------------------------------
 struct Shape {
-  uint32_t rows;     // of a tile
-  uint32_t workers;  // workgroups: as many as the device holds at a time
+  uint32_t waves;      // of a workgroup; 0: k_attend16, else k_attend32 with so many
+  uint32_t workers;    // workgroups: as many as the device holds at a time
+  uint32_t slot_rows;
+  Kind kind[2];
+  uint32_t few;
 };
+
+Kind kind_of(const tl_ctx* ctx, uint32_t group, uint32_t rows) {
+  Kind k;
+  k.rows = rows;
+  k.parts = (group + rows - 1) / rows;
+  k.part_heads = (group + k.parts - 1) / k.parts;
+  k.tile_rows = rows / k.part_heads;
+  return k;
+}
 
 Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
   Shape s;
-  const uint64_t per = n_rows * (n_q_heads / ctx->H) / (n_reqs ? n_reqs : 1);
-  s.rows = per <= 32 ? 16 : 128;
-  s.workers = ctx->D == 256 ? 256 : 512;
+  const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
+  const uint64_t per = n_rows * group / (n_reqs ? n_reqs : 1);
+  s.waves = per <= 32 ? 0 : ctx->D == 256 || per <= 128 ? 4 : 8;
+  s.workers = ctx->D == 256 || s.waves == 8 ? 256 : 512;
+  s.few = s.waves ? 32 / group : ~0u;
+  Kind& f = s.kind[0];
+  f = kind_of(ctx, group, 16);
+  const uint32_t runs = ctx->H * f.parts;
+  f.heads_shift = 0;
+  while ((2u << f.heads_shift) <= (s.waves ? s.waves : 4) && runs % (2u << f.heads_shift) == 0) ++f.heads_shift;
+  f.heads = runs >> f.heads_shift;
+  // keys of a wavefront's step, and how many wavefronts take steps of one run
+  f.block_shift = (ctx->D * wide < 128 ? 6 : 5) + (s.waves == 8 ? 3 : 2) - f.heads_shift;
+  Kind& m = s.kind[1];
+  m = kind_of(ctx, group, 32 * (s.waves ? s.waves : 4));
+  m.heads_shift = 0;
+  m.heads = ctx->H * m.parts;
+  m.block_shift = ctx->D == 256 ? 5 : 6;
+  s.slot_rows = 16u << f.heads_shift;
+  if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
   return s;
 }
 
@@ -909,26 +1182,35 @@ struct Layout {
 };
 Layout layout_of(const Shape& s, uint32_t D) {
   Layout l;
+  const uint64_t rows = 2ull * s.workers * s.slot_rows;
   l.ml = ((uint64_t)s.workers * sizeof(Share) + 255) / 256 * 256;
-  l.o = l.ml + 2ull * s.workers * s.rows * 2 * 4;
-  l.end = l.o + 2ull * s.workers * s.rows * D * 4;
+  l.o = l.ml + rows * 2 * 4;
+  l.end = l.o + rows * D * 4;
   return l;
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool EVEN>
 void launch(const Shape& sh, hipStream_t s, const AttendArgs& a) {
   {
     TimedLaunch timed(TL_KERNEL_ATTEND, s);
-    if (sh.rows == 16)
-      hipLaunchKernelGGL((k_attend16<D, FP8>), dim3(sh.workers), dim3(kThreads), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_attend128<D, FP8>), dim3(sh.workers), dim3(kThreads), 0, s, a);
+    const dim3 grid(sh.workers);
+    if (!sh.waves)
+      hipLaunchKernelGGL((k_attend16<D, FP8, EVEN>), grid, dim3(256), 0, s, a);
+    else if (sh.waves == 4)
+      hipLaunchKernelGGL((k_attend32<D, FP8, EVEN, 4>), grid, dim3(256), 0, s, a);
+    else if constexpr (D != 256)
+      hipLaunchKernelGGL((k_attend32<D, FP8, EVEN, 8>), grid, dim3(512), 0, s, a);
   }
   TimedLaunch timed(TL_KERNEL_ATTEND_JOIN, s);
-  if (sh.rows == 16)
-    hipLaunchKernelGGL((k_attend_join<16, D>), dim3(sh.workers - 1), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((k_attend_join<D>), dim3((sh.workers - 1) * (a.slot_rows * D / 1024)), dim3(256), 0, s, a);
+}
+
+template <int D>
+void launch(bool fp8, bool even, const Shape& sh, hipStream_t s, const AttendArgs& a) {
+  if (fp8)
+    even ? launch<D, true, true>(sh, s, a) : launch<D, true, false>(sh, s, a);
   else
-    hipLaunchKernelGGL((k_attend_join<128, D>), dim3(sh.workers - 1), dim3(kThreads), 0, s, a);
+    even ? launch<D, false, true>(sh, s, a) : launch<D, false, false>(sh, s, a);
 }
 
 }  // namespace
@@ -952,23 +1234,26 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
   a.n_heads = ctx->H;
   a.group = n_q_heads / ctx->H;
   const Shape sh = shape_of(ctx, n_q_heads, batch->n_reqs, batch->n_rows);
-  a.parts = (a.group + sh.rows - 1) / sh.rows;
-  a.part_heads = (a.group + a.parts - 1) / a.parts;
-  a.tile_rows = sh.rows / a.part_heads;
+  a.kind[0] = sh.kind[0];
+  a.kind[1] = sh.kind[1];
+  a.few = sh.few;
+  a.slot_rows = sh.slot_rows;
   a.all = (flags & TL_ATTEND_ALL) != 0;
   a.window = a.all ? 0 : (uint32_t)ctx->window[layer];
-  a.scale = scale * 1.4426950408889634f;
+  const float by = scale * 1.4426950408889634f;
+  a.scale = fmaxf(fabsf(by), 1e-37f);
+  a.q_sign = by < 0.f ? 0x80008000u : 0u;
   const Layout lay = layout_of(sh, ctx->D);
   a.share = (Share*)d_ws;
   a.part_ml = (float*)((uint8_t*)d_ws + lay.ml);
   a.part_o = (float*)((uint8_t*)d_ws + lay.o);
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
-  const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED;
+  const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED, even = ctx->P % 16 == 0;
   switch (ctx->D) {
-    case 64: fp8 ? launch<64, true>(sh, s, a) : launch<64, false>(sh, s, a); break;
-    case 128: fp8 ? launch<128, true>(sh, s, a) : launch<128, false>(sh, s, a); break;
-    default: fp8 ? launch<256, true>(sh, s, a) : launch<256, false>(sh, s, a); break;
+    case 64: launch<64>(fp8, even, sh, s, a); break;
+    case 128: launch<128>(fp8, even, sh, s, a); break;
+    default: launch<256>(fp8, even, sh, s, a); break;
   }
   return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE;
 }

@@ -81,11 +81,16 @@ class tl_rope(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
+_BF16 = None  # torch's bf16, where torch is there
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError("libtaliesin.so is not built (python -m paper_2609_39358_amd.build)")
+    global _BF16
     try:  # bind the library's HIP calls to the runtime torch has already loaded
-        import torch  # noqa: F401
+        import torch
+        _BF16 = torch.bfloat16
     except ImportError:
         pass
     lib = ctypes.CDLL(LIB_PATH)
@@ -221,6 +226,7 @@ class Ctx:
         _check(_lib.tl_ctx_geometry(handle, ctypes.byref(g)), "tl_ctx_geometry")
         for name, _ in tl_geometry._fields_:
             setattr(self, name, int(getattr(g, name)))
+        self.layer_bytes = 8 * (self.n_slabs // (2 * self.pages_per_block))  # of an array of layer addresses
 
     @property
     def handle(self) -> int:
@@ -315,6 +321,8 @@ def tl_block_keys_batch(ctx: Ctx, docs: Sequence, parents=None, block_bytes: int
 def make_cache(d_layer_k, d_layer_v, page_stride: int, n_pages: int) -> tl_cache:
     c = tl_cache(_addr(d_layer_k), _addr(d_layer_v), page_stride, n_pages)
     c._keep = (d_layer_k, d_layer_v)  # the buffers must outlive the enqueued kernels
+    # bytes of both that every call may count on (0: looked at in each call)
+    c._room = min(x.nbytes if getattr(x, "is_cuda", False) and x.is_contiguous() else 0 for x in c._keep)
     return c
 
 
@@ -356,7 +364,7 @@ def _check_blocks(ctx: Ctx, n: int, blocks: tl_blocks):
 
 def _check_cache(ctx: Ctx, cache: tl_cache):
     keep = getattr(cache, "_keep", None)
-    if keep is None:
+    if keep is None or cache._room >= ctx.layer_bytes:
         return
     n_layers = ctx.n_slabs // (2 * ctx.pages_per_block)
     _fits(keep[0], 8 * n_layers, "K layer addresses")
@@ -599,23 +607,24 @@ def make_rope(d_cos_sin, rot_dim: int, d_pos=None, pair_axis: Optional[Sequence[
     return r
 
 
-def _rows(x, batch: tl_batch, dim: Optional[int], what: str) -> tl_rows:
+def _rows(x, n_rows: int, dim: int, what: str) -> tl_rows:
     """A bf16 device tensor [n_rows, heads, head_dim] whose last dimension is
     contiguous; any other strides that are multiples of 8."""
-    if x.dtype.itemsize != 2 or "bfloat16" not in str(x.dtype):
+    shape, stride = x.shape, x.stride()
+    if x.dtype is not _BF16:
         raise ValueError("%s must be bf16, got %s" % (what, x.dtype))
-    if x.device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError("%s must be device memory, got a %s tensor" % (what, x.device.type))
-    if x.dim() != 3 or x.shape[0] != batch.n_rows or (dim is not None and x.shape[2] != dim):
-        raise ValueError("%s has shape %s for %d rows" % (what, tuple(x.shape), batch.n_rows))
-    if x.stride(2) != 1:
+    if len(shape) != 3 or shape[0] != n_rows or shape[2] != dim:
+        raise ValueError("%s has shape %s for %d rows" % (what, tuple(shape), n_rows))
+    if stride[2] != 1:
         raise ValueError("%s must be contiguous in its last dimension" % what)
-    return tl_rows(x.data_ptr(), x.stride(0), x.stride(1))
+    return tl_rows(x.data_ptr(), stride[0], stride[1])
 
 
 def _check_operator(ctx: Ctx, batch: tl_batch, cache: tl_cache):
     keep = getattr(batch, "_keep", None)
-    if keep is not None:
+    if keep is not None and ctx.n_groups > 1:
         _fits(keep[2], 4 * ctx.n_groups * batch.n_reqs * batch.table_width, "page tables")
     _check_cache(ctx, cache)
 
@@ -625,18 +634,22 @@ def tl_append(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, k,
     """Rotates and appends the rows' keys and values [n_rows, n_kv_heads,
     head_dim] to the cache's pages, and rotates the queries q into q_out."""
     _check_operator(ctx, batch, cache)
+    n, dim, heads = batch.n_rows, ctx.head_dim, 0
     if k.shape[1] != ctx.n_kv_heads or v.shape[1] != ctx.n_kv_heads:
         raise ValueError("keys and values of %d and %d heads for a cache of %d" % (k.shape[1], v.shape[1], ctx.n_kv_heads))
-    if (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
-        raise ValueError("queries and rotated queries go together and have one shape")
-    _fits(d_status, batch.n_rows, "status")
-    if rope is not None and getattr(rope, "_keep", None) is not None:
-        _fits(rope._keep[1], 4 * rope.n_axes * batch.n_rows, "positions")
-    rows = lambda x, what: None if x is None else ctypes.byref(_rows(x, batch, ctx.head_dim, what))  # noqa: E731
-    _check(_lib.tl_append(ctx.handle, _stream(stream), layer, ctypes.byref(batch),
-                          None if rope is None else ctypes.byref(rope), rows(k, "keys"), rows(v, "values"),
-                          0 if q is None else q.shape[1], rows(q, "queries"), rows(q_out, "rotated queries"),
-                          ctypes.byref(cache), _addr(d_status)), "tl_append")
+    if q is not None or q_out is not None:
+        if q is None or q_out is None or q.shape != q_out.shape:
+            raise ValueError("queries and rotated queries go together and have one shape")
+        heads, q, q_out = q.shape[1], _rows(q, n, dim, "queries"), _rows(q_out, n, dim, "rotated queries")
+    _fits(d_status, n, "status")
+    if rope is not None:
+        keep = getattr(rope, "_keep", None)
+        if keep is not None and keep[1] is not None:
+            _fits(keep[1], 4 * rope.n_axes * n, "positions")
+    st = _lib.tl_append(ctx.handle, _stream(stream), layer, batch, rope, _rows(k, n, dim, "keys"), _rows(v, n, dim, "values"),
+                        heads, q, q_out, cache, _addr(d_status))
+    if st:
+        _check(st, "tl_append")
 
 
 def tl_attend_workspace_bytes(ctx: Ctx, n_q_heads: int, n_reqs: int, n_rows: int) -> int:
@@ -648,15 +661,16 @@ def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q,
     """Attention of q [n_rows, n_q_heads, head_dim] over the cache into out;
     scale: head_dim ** -0.5 by default; all_keys: TL_ATTEND_ALL."""
     _check_operator(ctx, batch, cache)
-    if q.shape != out.shape:
-        raise ValueError("queries %s and results %s differ in shape" % (tuple(q.shape), tuple(out.shape)))
-    _fits(lse, 4 * batch.n_rows * q.shape[1], "lse")
+    n, dim, shape = batch.n_rows, ctx.head_dim, q.shape
+    if shape != out.shape:
+        raise ValueError("queries %s and results %s differ in shape" % (tuple(shape), tuple(out.shape)))
+    _fits(lse, 4 * n * shape[1], "lse")
     _fits(d_workspace, workspace_bytes, "workspace")
-    _check(_lib.tl_attend(ctx.handle, _stream(stream), layer, ctypes.byref(batch), q.shape[1],
-                          ctypes.byref(_rows(q, batch, ctx.head_dim, "queries")), ctypes.byref(cache),
-                          ctx.head_dim ** -0.5 if scale is None else scale, TL_ATTEND_ALL if all_keys else 0,
-                          ctypes.byref(_rows(out, batch, ctx.head_dim, "results")), _addr(lse), _addr(d_workspace),
-                          workspace_bytes), "tl_attend")
+    st = _lib.tl_attend(ctx.handle, _stream(stream), layer, batch, shape[1], _rows(q, n, dim, "queries"), cache,
+                        dim ** -0.5 if scale is None else scale, TL_ATTEND_ALL if all_keys else 0,
+                        _rows(out, n, dim, "results"), _addr(lse), _addr(d_workspace), workspace_bytes)
+    if st:
+        _check(st, "tl_attend")
 
 
 # ------------------------------------------------------------------ record files (disk tier)
