@@ -31,6 +31,10 @@ struct AppendArgs {
 
 constexpr int kWaves = 4;
 
+typedef __attribute__((address_space(1))) uint8_t* GlobalOut;
+typedef __attribute__((address_space(1))) u32x2* GlobalOut2;
+typedef __attribute__((address_space(1))) u32x4* GlobalOut4;
+
 // A row of D elements is held by D / 16 lanes, 16 elements each: x[0..8) and
 // x[8..16) are the two halves of eight pairs, or two runs of eight elements.
 template <int D>
@@ -182,7 +186,7 @@ __device__ void put_fragment(const AppendArgs& a, uint32_t t, uint32_t n, uint32
     const bool is_k = (job & 1) == 0;
     const uint32_t head = (job >> 1) * heads + row / span;
     const Rows& in = is_k ? a.k : a.v;
-    uint8_t* base = (uint8_t*)(is_k ? *a.c.k : *a.c.v) + (int64_t)page * a.c.stride;
+    GlobalOut base = (GlobalOut)*(is_k ? a.c.k : a.c.v) + (int64_t)page * a.c.stride;
     if (!FP8) {
       if (head < a.n_heads) {
         uint32_t first, second;
@@ -190,9 +194,9 @@ __device__ void put_fragment(const AppendArgs& a, uint32_t t, uint32_t n, uint32
         for (uint32_t i = sub; i < n; i += span) {
           float x[16];
           load_row(a, in, is_k, t + i, head, position + i, j, x);
-          uint16_t* out = (uint16_t*)base + ((uint64_t)(o + i) * a.n_heads + head) * D;
-          *(u32x4*)(out + first) = pack(x);
-          *(u32x4*)(out + second) = pack(x + 8);
+          const GlobalOut out = base + ((uint64_t)(o + i) * a.n_heads + head) * (2 * D);
+          *(GlobalOut4)(out + 2 * first) = pack(x);
+          *(GlobalOut4)(out + 2 * second) = pack(x + 8);
         }
       }
       continue;
@@ -207,14 +211,14 @@ __device__ void put_fragment(const AppendArgs& a, uint32_t t, uint32_t n, uint32
     for (uint32_t k = 1; k < L * span; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
     if (head >= a.n_heads) continue;
     uint32_t b = scale_byte(m);
-    uint8_t* scales = base + a.c.scale_off;
+    const GlobalOut scales = base + a.c.scale_off;
     if (o) {
       const uint32_t old = scale_held(scales[head]);
       if (b > old) {
         // the page's scale rises: the rows before are rounded again
         const float by = scale_inverse(127 + min(b - old, 40u));  // 2^(old - b); 448 * 2^-40 rounds to 0 as well
         for (uint32_t i = sub; i < o; i += span) {
-          u32x4* p = (u32x4*)(base + ((uint64_t)i * a.n_heads + head) * D + 16 * j);
+          const GlobalOut4 p = (GlobalOut4)(base + ((uint64_t)i * a.n_heads + head) * D + 16 * j);
           u32x4 w = *p;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -235,9 +239,9 @@ __device__ void put_fragment(const AppendArgs& a, uint32_t t, uint32_t n, uint32
     for (uint32_t i = sub; i < n; i += span) {
       float x[16];
       load_row(a, in, is_k, t + i, head, position + i, j, x);
-      uint8_t* out = base + ((uint64_t)(o + i) * a.n_heads + head) * D;
-      *(u32x2*)(out + first) = codes8(x, inv);
-      *(u32x2*)(out + second) = codes8(x + 8, inv);
+      const GlobalOut out = base + ((uint64_t)(o + i) * a.n_heads + head) * D;
+      *(GlobalOut2)(out + first) = codes8(x, inv);
+      *(GlobalOut2)(out + second) = codes8(x + 8, inv);
     }
   }
 }

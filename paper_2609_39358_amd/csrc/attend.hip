@@ -82,6 +82,17 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
   return q;
 }
 
+// What a whole workgroup works on, in scalar registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x);
+}
+__device__ __forceinline__ Request uniform(Request q) {
+  return Request{uniform(q.row0), uniform(q.rows), uniform(q.tiles), uniform(q.held), uniform(q.before),
+                 uniform(q.kind), uniform(q.tile_rows), uniform(q.heads), uniform(q.block_shift)};
+}
+
 struct Span {
   int lo, hi;      // keys [lo, hi) are seen by some row of the tile
   uint32_t b0, n;  // blocks of keys from b0 on; at least one, so that every tile has a worker
@@ -164,7 +175,7 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   }
   if (tid == 0) l.found = ~0u;
   __syncthreads();
-  c.total = l.sum[kPlan];
+  c.total = uniform(l.sum[kPlan]);
   c.workers = (uint32_t)min((uint64_t)gridDim.x, c.total);
   // runs that follow each other go to workgroups of one chiplet, which share an L2
   c.worker = blockIdx.x;
@@ -179,12 +190,12 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
     l.found_at = l.sum[tid];
   }
   __syncthreads();
-  if (l.found == ~0u) return false;
-  c.r = __builtin_amdgcn_readfirstlane(l.found);
-  c.first = l.found_at;
+  c.r = uniform(l.found);
+  if (c.r == ~0u) return false;
+  c.first = uniform(l.found_at);
   while (c.r < n) {
-    const Request q = request_of(a, c.r);
-    const uint64_t blocks = split > 1 ? (l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : blocks_of(a, q, 0, 1);
+    const Request q = uniform(request_of(a, c.r));
+    const uint64_t blocks = split > 1 ? uniform(l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : blocks_of(a, q, 0, 1);
     if (c.at < c.first + blocks * q.heads) {
       c.head = (uint32_t)((c.at - c.first) / blocks);
       c.first += c.head * blocks;
@@ -305,7 +316,7 @@ struct Tile16 {
   static constexpr int kVWords = FP8 ? kElems / 4 : kElems / 2;
   uint32_t k[2 * kGroups][kKWords];
   uint32_t v[8 * kGroups][kVWords];
-  float k_scale[2 * kGroups], v_scale[8 * kGroups];
+  uint32_t ks, vs;  // a lane's key's (or sixteen keys') words of scale bytes
   uint64_t seen;  // which of the keys are to be used
 };
 
@@ -334,25 +345,25 @@ __device__ __forceinline__ int64_t lane_value(int64_t x, uint32_t lane) {
 }
 
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t* w, const uint8_t* p) {
+__device__ __forceinline__ void load_words(uint32_t* w, GlobalBytes p) {
   if constexpr (N >= 4) {
 #pragma unroll
     for (int k = 0; k < N / 4; ++k) {
-      const u32x4 x = *(const u32x4*)(p + 16 * k);
+      const u32x4 x = *(GlobalU32x4)(p + 16 * k);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[4 * k + j] = x[j];
     }
   } else if constexpr (N == 2) {
-    const u32x2 x = *(const u32x2*)p;
+    const u32x2 x = *(GlobalU32x2)p;
     w[0] = x[0];
     w[1] = x[1];
   } else {
-    w[0] = *(const uint32_t*)p;
+    w[0] = *(GlobalU32)p;
   }
 }
 
 template <int D, bool FP8, bool EVEN>
-__device__ __forceinline__ void load16(const AttendArgs& a, const uint8_t* kp, const uint8_t* vp, uint32_t kv, const Ids16& id,
+__device__ __forceinline__ void load16(const AttendArgs& a, GlobalBytes kp, GlobalBytes vp, uint32_t kv, const Ids16& id,
                                        Tile16<D, FP8>& t) {
   typedef Tile16<D, FP8> Tile;
   constexpr uint32_t kRow = FP8 ? D : 2 * D;  // bytes of a head's row
@@ -363,33 +374,29 @@ __device__ __forceinline__ void load16(const AttendArgs& a, const uint8_t* kp, c
   const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
   const uint32_t step = a.n_heads * kRow;  // bytes from a key to the next
   const int64_t off = page + (fine ? (int64_t)id.row * step : 0) + (int64_t)kv * kRow;
-  uint32_t ks = 127, vs = 127;
   if (FP8) {
-    const int64_t at = page + a.c.scale_off + kv;
-    ks = scale_held(kp[at]);
-    vs = scale_held(vp[at]);
+    t.ks = scale_word(kp + page, a.c.scale_off, kv);
+    t.vs = scale_word(vp + page, a.c.scale_off, kv);
   }
 #pragma unroll
   for (int h = 0; h < 2 * Tile::kGroups; ++h) {
-    const uint8_t* p;
+    GlobalBytes p;
     if constexpr (EVEN)
       p = kp + lane_value(off, h * 16) + (c * step + 16 * quad);
     else
       p = kp + __shfl(off, h * 16 + c) + 16 * quad;
 #pragma unroll
     for (int i = 0; i < Tile::kKWords / 4; ++i) load_words<4>(t.k[h] + 4 * i, p + 64 * i);
-    if (FP8) t.k_scale[h] = scale_value(EVEN ? __builtin_amdgcn_readlane(ks, h * 16) : __shfl(ks, h * 16 + c));
   }
 #pragma unroll
   for (int i = 0; i < 8 * Tile::kGroups; ++i) {
     const uint32_t key = quad * 4 + i % 4, half = i / 4 * 16;
-    const uint8_t* p;
+    GlobalBytes p;
     if constexpr (EVEN)
       p = vp + lane_value(off, half) + (key * step + kRow / 16 * c);
     else
       p = vp + __shfl(off, half + key) + kRow / 16 * c;
     load_words<Tile::kVWords>(t.v[i], p);
-    if (FP8) t.v_scale[i] = scale_value(EVEN ? __builtin_amdgcn_readlane(vs, half) : __shfl(vs, half + key));
   }
 }
 
@@ -400,12 +407,24 @@ struct Rows16 {
   Soft s;
 };
 
-template <int D, bool FP8>
-__device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, int key0, const Place& p, bool edge,
+template <int D, bool FP8, bool EVEN>
+__device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, uint32_t kv, int key0, const Place& p, bool edge,
                                         Rows16<D, FP8>& r) {
   typedef Tile16<D, FP8> Tile;
   constexpr int N = 8 * Tile::kGroups;
-  const uint32_t quad = (threadIdx.x & 63) / 16;
+  const uint32_t lane = threadIdx.x & 63, c = lane % 16, quad = lane / 16;
+  float k_scale[2 * Tile::kGroups], v_scale[EVEN ? 2 * Tile::kGroups : N];
+  if constexpr (FP8) {
+    const uint32_t kb = scale_held(scale_of(t.ks, kv)), vb = scale_held(scale_of(t.vs, kv));
+#pragma unroll
+    for (int h = 0; h < 2 * Tile::kGroups; ++h) {
+      k_scale[h] = scale_value(EVEN ? __builtin_amdgcn_readlane(kb, h * 16) : __shfl(kb, h * 16 + c));
+      if constexpr (EVEN) v_scale[h] = scale_value(__builtin_amdgcn_readlane(vb, h * 16));
+    }
+    if constexpr (!EVEN)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v_scale[i] = scale_value(__shfl(vb, i / 4 * 16 + quad * 4 + i % 4));
+  }
   float x[N];
 #pragma unroll
   for (int h = 0; h < 2 * Tile::kGroups; ++h) {
@@ -414,10 +433,10 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
     for (int k = 0; k < D / 32; ++k) {
       u32x4 w;
       if constexpr (FP8) {
-        w[0] = widen(t.k[h][2 * k], t.k_scale[h], false);
-        w[1] = widen(t.k[h][2 * k], t.k_scale[h], true);
-        w[2] = widen(t.k[h][2 * k + 1], t.k_scale[h], false);
-        w[3] = widen(t.k[h][2 * k + 1], t.k_scale[h], true);
+        w[0] = widen(t.k[h][2 * k], k_scale[h], false);
+        w[1] = widen(t.k[h][2 * k], k_scale[h], true);
+        w[2] = widen(t.k[h][2 * k + 1], k_scale[h], false);
+        w[3] = widen(t.k[h][2 * k + 1], k_scale[h], true);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = t.k[h][4 * k + j];
@@ -470,7 +489,7 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if constexpr (FP8)
-          e[i] = widen(t.v[8 * g + i][n / 4], t.v_scale[8 * g + i], n & 2);
+          e[i] = widen(t.v[8 * g + i][n / 4], v_scale[EVEN ? 2 * g + i / 4 : 8 * g + i], n & 2);
         else
           e[i] = t.v[8 * g + i][n / 2];
       }
@@ -503,8 +522,7 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), c = lane % 16, quad = lane / 16;
   const uint32_t hs = kind.heads_shift, heads = 1u << hs;
   const int step = 1 << kind.block_shift;  // keys of a block
-  const uint8_t* kp = (const uint8_t*)*a.c.k;
-  const uint8_t* vp = (const uint8_t*)*a.c.v;
+  const GlobalBytes kp = layer_base(a.c.k), vp = layer_base(a.c.v);
   const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
   const uint32_t head = (cur.head << hs) + (wave & (heads - 1)), sub = wave >> hs;
   const uint32_t kv = head / kind.parts;
@@ -535,11 +553,11 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     for (int key = key0; key <= last; key += 2 * step) {
       load16<D, FP8, EVEN>(a, kp, vp, kv, id, tb);
       id = ids16<EVEN>(a, table, min(key + 2 * step, last) + mine, s);
-      block16<D, FP8>(a, ta, key, p, edge(key), r);
+      block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), r);
       if (key + step > last) break;
       load16<D, FP8, EVEN>(a, kp, vp, kv, id, ta);
       id = ids16<EVEN>(a, table, min(key + 3 * step, last) + mine, s);
-      block16<D, FP8>(a, tb, key + step, p, edge(key + step), r);
+      block16<D, FP8, EVEN>(a, tb, kv, key + step, p, edge(key + step), r);
     }
   }
 
@@ -621,7 +639,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a
     return;
   }
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Request q = request_of(a, cur.r);
+    const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
     const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s);
@@ -651,12 +669,10 @@ struct Lds32 {
   static constexpr int KT = D == 256 ? 32 : 64;  // keys of a block
   alignas(1024) uint16_t k[2][KT * D];
   uint16_t v[2][KT * D];
-  int64_t off[4][KT];     // byte offsets of the keys' rows
-  uint32_t scale[4][KT];  // scale bytes: K's, and V's in bits 8 to 15; 0: not to be used
-  uint64_t seen[4];       // keys that are to be used
 };
 
 typedef __attribute__((address_space(3))) const char* LdsAddress;
+typedef __attribute__((address_space(3))) u32x4* LdsU32x4;
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsAddress)p; }
 
 // Where an element is kept: such that lanes that read or write together use all
@@ -683,31 +699,31 @@ template <int D, bool FP8, int WAVES>
 __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, const Cursor& cur, const Request& q, const Span& s,
                                           uint32_t k0, uint32_t k1) {
   constexpr int KT = Lds32<D>::KT, NB = KT / 32, kThreads = 64 * WAVES;
-  constexpr int kRow = FP8 ? D : 2 * D;                             // bytes of a head's row
-  constexpr int kPieces = kRow / 16;                                // 16-byte pieces of a key
-  constexpr int kLoads = (KT * kPieces + kThreads - 1) / kThreads;  // of K (and of V) per thread
-  constexpr bool kSpare = KT * kPieces % kThreads != 0;             // some threads have none
-  constexpr uint32_t kBatch = 4, kDs = D == 64 ? 2 : 4;             // products whose operands are read at a time
-  constexpr uint64_t kAllSeen = KT == 64 ? ~0ull : 0xffffffffull;
+  constexpr int kRow = FP8 ? D : 2 * D;                    // bytes of a head's row
+  constexpr int kPieces = kRow / 16;                       // 16-byte pieces of a key
+  constexpr int kKeys = kThreads / kPieces;                // keys that the threads bring at a time
+  constexpr int kLoads = KT < kKeys ? 1 : KT / kKeys;      // pieces of K (and of V) per thread
+  constexpr int kWaveKeys = 64 / kPieces;                  // keys of a wavefront at a time
+  constexpr uint32_t kBatch = 4, kDs = D == 64 ? 2 : 4;    // products whose operands are read at a time
   const Kind& kind = a.kind[1];
   const uint32_t tid = threadIdx.x, lane = tid & 63, c = lane % 32, half = lane / 32;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
-  const uint8_t* kp = (const uint8_t*)*a.c.k;
-  const uint8_t* vp = (const uint8_t*)*a.c.v;
+  const GlobalBytes kp = layer_base(a.c.k), vp = layer_base(a.c.v);
   const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
   const uint32_t kv = cur.head / kind.parts;
 
   const uint32_t m = wave * 32 + c;
-  const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
   bf16x8 qf[D / 16];
-  {
-    const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) qf[k] = load_q(a, qp + k * 16 + half * 8, p.there);
-  }
+  int row_lo, row_hi;  // keys that this lane's row sees
   // keys that some row of this wavefront sees, and keys that all of them see
   int wave_lo, wave_hi, all_lo, all_hi;
   {
+    const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
+    const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) qf[k] = load_q(a, qp + k * 16 + half * 8, p.there);
+    row_lo = p.lo;
+    row_hi = p.hi;
     int lo = p.there ? p.lo : 0x7fffffff, hi = p.there ? p.hi : 0, lo2 = p.there ? p.lo : 0, hi2 = p.there ? p.hi : 0x7fffffff;
     for (uint32_t k = 1; k < 32; k *= 2) {
       lo = min(lo, __shfl_xor(lo, k));
@@ -715,10 +731,10 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
       lo2 = max(lo2, __shfl_xor(lo2, k));
       hi2 = min(hi2, __shfl_xor(hi2, k));
     }
-    wave_lo = __builtin_amdgcn_readfirstlane(lo);
-    wave_hi = __builtin_amdgcn_readfirstlane(hi);
-    all_lo = __builtin_amdgcn_readfirstlane(lo2);
-    all_hi = __builtin_amdgcn_readfirstlane(hi2);
+    wave_lo = uniform(lo);
+    wave_hi = uniform(hi);
+    all_lo = uniform(lo2);
+    all_hi = uniform(hi2);
   }
   f32x16 o[D / 32];
 #pragma unroll
@@ -727,84 +743,98 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   Soft st = {kNone, 0.f, 0.f};
 
-  const int blocks = (int)(k1 - k0), block0 = (int)(s.b0 + k0) * KT, block_last = (int)(s.b0 + k1 - 1) * KT;
+  const int blocks = (int)(k1 - k0), block0 = (int)(s.b0 + k0) * KT;
+  const uint32_t step = a.n_heads * kRow;  // bytes from a key to the next
+  // whether a page of these blocks is missing (rare: then every key is asked)
+  bool holes = false;
+  if (s.hi > s.lo) {
+    const uint32_t first = a.b.page.div((uint32_t)max(s.lo, block0)), last = a.b.page.div((uint32_t)min(s.hi, block0 + blocks * KT) - 1);
+    int gone = 0;
+    for (uint32_t i = first + tid; i <= last; i += kThreads) gone |= (uint32_t)table[i] >= a.c.n_pages;
+    holes = __syncthreads_or(gone);
+  }
+  // What a thread brings: a 16-byte piece of K and V of kLoads keys of a block.
+  // Keys that no row sees are read from the nearest one that some row does.
+  const uint32_t piece = lane / kWaveKeys, my_key = wave * kWaveKeys + lane % kWaveKeys;
+  const bool brings = my_key < KT;
+  static_assert(kKeys % (D == 64 ? 16 : 8) == 0, "a later key's place differs by an exclusive or alone");
+  const uint32_t k_to = lds_of(l.k[0]) + k_at<D>(my_key, FP8 ? 2 * piece : piece) * 2;
+  const uint32_t v_to = lds_of(l.v[0]) + v_at<D>(my_key, (FP8 ? 16 : 8) * piece) * 2;
   u32x4 kr[kLoads], vr[kLoads];
-  // wavefront 0: where the keys of block n are
-  auto find = [&](int n, Ids16& id) {
-    if (wave == 0) id = ids16<false>(a, table, min(block0 + n * KT, block_last) + (int)(lane % KT), s);
-  };
-  auto scales = [&](const Ids16& id, uint32_t& ks, uint32_t& vs) {
-    if (!FP8 || wave != 0) return;
-    const int64_t at = (id.in && id.page < a.c.n_pages ? (int64_t)id.page * a.c.stride : 0) + a.c.scale_off + kv;
-    ks = kp[at];
-    vs = vp[at];
-  };
-  auto note = [&](const Ids16& id, uint32_t ks, uint32_t vs, uint32_t n) {
-    if (wave != 0) return;
-    const uint32_t slot = n & 3;
-    const bool fine = id.in && id.page < a.c.n_pages;
-    const int64_t page = fine ? (int64_t)id.page * a.c.stride : 0;
-    uint32_t sc = 0x7f7f;
-    if (FP8) sc = scale_held(ks) | scale_held(vs) << 8;
-    const uint64_t seen = __ballot(fine);
-    if (KT == 64 || lane < KT) {
-      l.off[slot][lane] = page + (fine ? (int64_t)id.row * a.n_heads * kRow : 0) + (int64_t)kv * kRow;
-      l.scale[slot][lane] = fine ? sc : 0;
-    }
-    if (lane == 0) l.seen[slot] = KT == 64 ? seen : seen & kAllSeen;
-  };
-  // a thread's pieces of block n, on their way from memory, and into shared memory
-  auto fetch = [&](u32x4* to, const uint8_t* from, uint32_t n) {
+  uint32_t page[kLoads], row[kLoads];       // of a block to come
+  int64_t k_off[kLoads];                    // of the block whose K is on its way
+  uint32_t k_word[kLoads], v_word[kLoads], v_next[kLoads];  // of scale bytes: V's of the block before K's, and of K's
+  uint32_t v_gone = 0, v_gone_next = 0;                     // whether its keys' pages are missing, a bit each
+  auto find = [&](int n) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
-      if (kSpare && row >= KT) continue;
-      to[i] = *(const u32x4*)(from + l.off[n & 3][row] + piece * 16);
+      const uint32_t key = (uint32_t)max(s.lo, min(block0 + n * KT + (int)my_key + i * kKeys, s.hi - 1)), at = a.b.page.div(key);
+      row[i] = key - at * a.b.page.d;
+      page[i] = (uint32_t)table[at];
     }
+  };
+  // K of the block that find() looked up, and its scales
+  auto fetch_k = [&]() {
+    v_gone = v_gone_next;
+    v_gone_next = 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const bool fine = page[i] < a.c.n_pages;
+      const int64_t base = fine ? (int64_t)page[i] * a.c.stride : 0;
+      k_off[i] = base + (int64_t)row[i] * step + (int64_t)kv * kRow + piece * 16;
+      kr[i] = *(GlobalU32x4)(kp + k_off[i]);
+      if (!fine) v_gone_next |= 1u << i;
+      if constexpr (FP8) {
+        v_word[i] = v_next[i];
+        k_word[i] = scale_word(kp + base, a.c.scale_off, kv);
+        v_next[i] = scale_word(vp + base, a.c.scale_off, kv);
+      }
+    }
+  };
+  // V of the block whose K was fetched last
+  auto fetch_v = [&]() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) vr[i] = *(GlobalU32x4)(vp + k_off[i]);
   };
   auto keep_k = [&](uint32_t n) {
-    uint16_t* to = l.k[n & 1];
+    if (!brings) return;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
-      if (kSpare && row >= KT) continue;
+      const uint32_t to = (k_to + ((n & 1) * KT + i * kKeys) * D * 2) ^ (k_swap<D>(i * kKeys) * 16);
       if constexpr (FP8) {
-        const float by = scale_value(l.scale[n & 3][row] & 0xff);
+        const float by = scale_value(scale_held(scale_of(k_word[i], kv)));
         u32x4 w[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           w[j / 2][j % 2 * 2] = widen(kr[i][j], by, false);
           w[j / 2][j % 2 * 2 + 1] = widen(kr[i][j], by, true);
         }
-        *(u32x4*)(to + k_at<D>(row, 2 * piece)) = w[0];
-        *(u32x4*)(to + k_at<D>(row, 2 * piece + 1)) = w[1];
+        *(LdsU32x4)(uintptr_t)to = w[0];
+        *(LdsU32x4)(uintptr_t)(to ^ 16) = w[1];
       } else {
-        *(u32x4*)(to + k_at<D>(row, piece)) = kr[i];
+        *(LdsU32x4)(uintptr_t)to = kr[i];
       }
     }
   };
   auto keep_v = [&](uint32_t n) {
-    uint16_t* to = l.v[n & 1];
-    const bool every = l.seen[n & 3] == kAllSeen;
+    if (!brings) return;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const uint32_t at = tid + i * kThreads, row = at / kPieces, piece = at % kPieces;
-      if (kSpare && row >= KT) continue;
-      const uint32_t sc = l.scale[n & 3][row];
+      const uint32_t to = v_to + ((n & 1) * KT + i * kKeys) * D * 2;
       u32x4 x = vr[i];
-      if (!every && !sc) x = u32x4{0, 0, 0, 0};  // whatever a page holds there, it may be NaN
+      if (holes && (v_gone >> i & 1)) x = u32x4{0, 0, 0, 0};  // whatever page 0 holds there, it may be NaN
       if constexpr (FP8) {
-        const float by = scale_value(sc >> 8);
+        const float by = scale_value(scale_held(scale_of(v_word[i], kv)));
         u32x4 w[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           w[j / 2][j % 2 * 2] = widen(x[j], by, false);
           w[j / 2][j % 2 * 2 + 1] = widen(x[j], by, true);
         }
-        *(u32x4*)(to + v_at<D>(row, 16 * piece)) = w[0];
-        *(u32x4*)(to + v_at<D>(row, 16 * piece + 8)) = w[1];
+        *(LdsU32x4)(uintptr_t)to = w[0];
+        *(LdsU32x4)(uintptr_t)(to ^ 16) = w[1];
       } else {
-        *(u32x4*)(to + v_at<D>(row, 8 * piece)) = x;
+        *(LdsU32x4)(uintptr_t)to = x;
       }
     }
   };
@@ -813,8 +843,14 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   // memory. The product's number goes in by an exclusive or, at the read itself:
   // one register each, not one for each product.
   const uint32_t k_lane = lds_of(l.k[0]) + c * D * 2 + (half ^ (k_swap<D>(c) & 1)) * 16 + k_swap<D>(c) / 2 * 32;
-  const uint32_t v_row = half * 4 + lane % 16 / 4;
-  const uint32_t v_lane = lds_of(l.v[0]) + v_row * D * 2 + ((lane / 16 % 2 * 16 + lane % 4 * 4) ^ v_swap<D>(v_row)) * 2;
+  auto v_lane = [&]() {
+    // the lane's number, asked for at every use: kept, this would be spilled, and
+    // waited for together with the loads on their way
+    uint32_t i;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(i));
+    const uint32_t v_row = i / 32 * 4 + i % 16 / 4;
+    return lds_of(l.v[0]) + v_row * D * 2 + ((i / 16 % 2 * 16 + i % 4 * 4) ^ v_swap<D>(v_row)) * 2;
+  };
   f32x16 x[NB];  // a block's scores
   bf16x8 w[2 * NB];  // and weights
 
@@ -827,7 +863,7 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
 #pragma unroll
       for (uint32_t j = 0; j < kBatch; ++j) {
         const uint32_t at = i * kBatch + j, b = at / (D / 16), k = at % (D / 16);
-        kf[i & 1][j] = *(__attribute__((address_space(3))) const u32x4*)((LdsAddress)(uintptr_t)(from ^ k * 32) + b * 32 * D * 2);
+        kf[i & 1][j] = *(LdsU32x4)((LdsAddress)(uintptr_t)(from ^ k * 32) + b * 32 * D * 2);
       }
     };
     read(0);
@@ -850,19 +886,24 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   // w = the weights of block n
   auto weigh = [&](uint32_t n) {
     const int key0 = block0 + (int)n * KT;
-    const uint64_t seen = l.seen[n & 3];
-    if (seen != kAllSeen || key0 < all_lo || key0 + KT > all_hi) {  // some row does not see some key
+    if (holes || key0 < all_lo || key0 + KT > all_hi) {  // some row may not see some key
+      const int first = key0 + 4 * (int)half;
+      uint32_t bits = ~0u;
+      if (holes)
+#pragma unroll 1
+        for (uint32_t t = 0; t < 16 * NB; ++t) {
+          const int key = first + (int)(t / 4 * 8 + t % 4);
+          const bool in = key >= row_lo && key < row_hi;
+          if (!in || (uint32_t)table[a.b.page.div((uint32_t)key)] >= a.c.n_pages) bits &= ~(1u << t);
+        }
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const uint32_t bits = (uint32_t)(seen >> (32 * b)) >> (4 * half);
-        const int first = key0 + 32 * b + 4 * (int)half;
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int at = 8 * (j / 4) + j % 4;
-          const bool there = (bits >> at & 1) && first + at >= p.lo && first + at < p.hi;
+          const int key = first + 32 * b + 8 * (j / 4) + j % 4;
+          const bool there = (bits >> (16 * b + j) & 1) && key >= row_lo && key < row_hi;
           x[b][j] = there ? x[b][j] : kNone;
         }
-      }
     }
     float top = x[0][0];
 #pragma unroll
@@ -892,7 +933,7 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   };
   // o += V^T w of block n, the operands read a batch ahead
   auto values = [&](uint32_t n) {
-    const uint32_t from = v_lane + (n & 1) * KT * D * 2;
+    const uint32_t from = v_lane() + (n & 1) * KT * D * 2;
     constexpr uint32_t kSteps = 2 * NB * (D / 32) / kDs;
     u32x2 vf[2][2 * kDs];
     auto read = [&](uint32_t i) {
@@ -922,47 +963,37 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   };
 
   if (s.hi > s.lo) {
-    // Block n is noted in slot n % 4 and kept in buffers n % 2. Past the last
-    // block the last one is read again.
-    Ids16 id, later;
-    uint32_t ks = 0, vs = 0;
+    // Block n is kept in buffers n % 2. Past the last block its last key is read
+    // again. Page ids are looked up a step before they are used.
     __syncthreads();
-#pragma unroll
-    for (int n = 0; n < 3; ++n) {
-      find(n, id);
-      scales(id, ks, vs);
-      note(id, ks, vs, n);
-    }
-    find(3, id);
-    __syncthreads();
-    fetch(kr, kp, 0);
-    keep_k(0);
+    find(0);
+    fetch_k();
+    find(1);
     if constexpr (WAVES == 8) {
-      // Wavefronts 0 to 3 are a phase ahead. A step of theirs keeps and fetches
-      // K of the next block and V of this one; the others', a phase later, those
-      // of the block after, so that all of it is there a phase before its use.
+      // Wavefronts 0 to 3 are a phase ahead. A step of theirs keeps K of the next
+      // block and V of this one; the others', a phase later, those of the block
+      // after, so that all of it is there a phase before its use.
       const uint32_t behind = wave / 4;
-      fetch(kr, kp, 1);
-      fetch(vr, vp, 0);
+      fetch_v();
+      keep_k(0);
+      fetch_k();
+      find(2);
       __syncthreads();
       if (used(0)) scores(0);
-      auto bring = [&](uint32_t n) {  // K of block n + 1 and V of block n into shared memory
+      auto bring = [&](uint32_t n) {
         keep_k(n + 1);
         keep_v(n);
-        fetch(kr, kp, n + 2);
-        fetch(vr, vp, n + 1);
+        fetch_v();
+        fetch_k();
+        find((int)n + 3);
       };
       if (behind) {
         bring(0);
         __syncthreads();
       }
       for (int n = 0; n < blocks; ++n) {
-        scales(id, ks, vs);
-        find(n + 4, later);
         if (used(n)) weigh(n);
         bring(n + behind);
-        note(id, ks, vs, n + 3);
-        id = later;
         __syncthreads();
         if (used(n)) values(n);
         if (n + 1 < blocks && used(n + 1)) scores(n + 1);
@@ -971,26 +1002,27 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
       if (!behind) __syncthreads();
     } else {
       // A step uses one block, keeps the next and fetches the one after.
-      fetch(vr, vp, 0);
-      keep_v(0);
-      fetch(kr, kp, 1);
-      fetch(vr, vp, 1);
+      auto bring = [&](uint32_t n) {
+        keep_k(n);
+        v_gone = v_gone_next;
+#pragma unroll
+        for (int i = 0; i < kLoads && FP8; ++i) v_word[i] = v_next[i];
+        keep_v(n);
+        fetch_k();
+        fetch_v();
+        find((int)n + 2);
+      };
+      fetch_v();
+      bring(0);
       __syncthreads();
       for (int n = 0; n < blocks; ++n) {
-        scales(id, ks, vs);
-        find(n + 4, later);
         const bool use = used(n);
         if (use) scores(n);
-        keep_k(n + 1);
-        keep_v(n + 1);
-        fetch(kr, kp, n + 2);
-        fetch(vr, vp, n + 2);
+        bring(n + 1);
         if (use) {
           weigh(n);
           values(n);
         }
-        note(id, ks, vs, n + 3);
-        id = later;
         __syncthreads();
       }
     }
@@ -998,6 +1030,7 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
 
   const float sum = st.sum + __shfl_xor(st.sum, 32);
   const bool whole = k0 == 0 && k1 == s.n;
+  const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
   if (p.there) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const uint64_t slot = (2 * (uint64_t)cur.worker + (k0 > 0 ? 0 : 1)) * a.slot_rows;
@@ -1037,7 +1070,7 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend32(Atten
     return;
   }
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Request q = request_of(a, cur.r);
+    const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
     const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s);

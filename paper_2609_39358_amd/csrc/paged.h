@@ -59,6 +59,15 @@ struct Pages {
   uint32_t scale_off;  // bytes of a page's codes: its scale bytes follow
 };
 
+// The caches' bases are read from memory: they are told apart from other address
+// spaces here, since a load that might be of shared memory is waited for with
+// every access to that.
+typedef __attribute__((address_space(1))) const uint8_t* GlobalBytes;
+typedef __attribute__((address_space(1))) const uint32_t* GlobalU32;
+typedef __attribute__((address_space(1))) const u32x2* GlobalU32x2;
+typedef __attribute__((address_space(1))) const u32x4* GlobalU32x4;
+__device__ __forceinline__ GlobalBytes layer_base(const uint64_t* p) { return (GlobalBytes)*p; }
+
 // Request that row t belongs to (first_row(r) <= t < first_row(r + 1)), or
 // n_reqs: found by the whole wavefront, 64 offsets at a time.
 __device__ __forceinline__ uint32_t find_request(const Batch& b, uint32_t t) {
@@ -83,6 +92,12 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
   const int b = (int)(bits >> 23) - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0);
   return (uint32_t)max(b, (int)kScaleMin);
 }
+// The word that holds a head's scale byte, which starts at bit 8 * (head % 4): in
+// a page the scales begin at a multiple of 64 bytes and end before its slab does.
+__device__ __forceinline__ uint32_t scale_word(GlobalBytes page, uint32_t scale_off, uint32_t head) {
+  return *(GlobalU32)(page + (scale_off + (head & ~3u)));
+}
+__device__ __forceinline__ uint32_t scale_of(uint32_t word, uint32_t head) { return word >> (8 * (head & 3)) & 0xff; }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254 - byte) << 23); }
 // A page's scale byte as it is used: one that no append writes is brought into range.
