@@ -652,21 +652,23 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a
   }
 }
 
-// ---- tiles of 32 rows for each wavefront ---------------------------------------------------
-// For prompts. A block of keys and values is widened to bf16 once, into shared
-// memory, and used by the 32 rows of each wavefront.
+// ---- tiles of many rows ---------------------------------------------------------------------
+// For prompts. A block of 64 keys and values is widened to bf16 once, into shared
+// memory, and used by the R rows of each wavefront.
 //
-// S^T = K Q^T with mfma 32x32x16: lane l takes row l % 32, and its result holds
-// keys 8 * (i / 4) + 4 * (l / 32) + i % 4. Registers 8a .. 8a + 7 are what the
-// lane gives to step a of O^T = V^T P^T, whose keys run in that order: V comes
-// from shared memory through transposing reads of four keys each.
+// S^T = K Q^T with mfma 32x32x16 (R = 32) or 16x16x32 (R = 16, for heads of 256,
+// whose 32 rows would not fit two wavefronts' registers on a SIMD): lane l takes
+// row l % R, and its result holds keys 8 * (i / 4) + 4 * (l / R) + i % 4 of R.
+// Eight of those registers at a time are what the lane gives to a step of
+// O^T = V^T P^T, whose keys run in that order: V comes from shared memory
+// through transposing reads of four keys each.
 //
 // With eight wavefronts two share a SIMD. They work in opposite phases, with a
 // barrier after each: while one wavefront's products (P V of this block, Q K of the
 // next) use the matrix unit, the other's exponentials use the vector unit.
 template <int D>
-struct Lds32 {
-  static constexpr int KT = D == 256 ? 32 : 64;  // keys of a block
+struct LdsMany {
+  static constexpr int KT = 64;  // keys of a block
   alignas(1024) uint16_t k[2][KT * D];
   uint16_t v[2][KT * D];
 };
@@ -674,6 +676,20 @@ struct Lds32 {
 typedef __attribute__((address_space(3))) const char* LdsAddress;
 typedef __attribute__((address_space(3))) u32x4* LdsU32x4;
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsAddress)p; }
+
+template <int R>
+struct Products;
+template <>
+struct Products<32> {
+  typedef f32x16 Sum;
+  static __device__ __forceinline__ Sum add(bf16x8 a, bf16x8 b, Sum c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Products<16> {
+  typedef f32x4 Sum;
+  static __device__ __forceinline__ Sum add(bf16x8 a, bf16x8 b, Sum c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+__host__ __device__ constexpr int rows_of_wave(int dim) { return dim == 256 ? 16 : 32; }
 
 // Where an element is kept: such that lanes that read or write together use all
 // banks. K: 8 neighbouring elements, chunk c of key r.
@@ -688,7 +704,7 @@ __device__ __forceinline__ uint32_t k_at(uint32_t r, uint32_t c) {
 // V: elem a multiple of 4.
 template <int D>
 __device__ __forceinline__ uint32_t v_swap(uint32_t r) {
-  return (D == 64 ? (r >> 1 & 1) : (r & 3)) * 32 + (r & 1) * 8;
+  return (D == 64 ? (r >> 1 & 1) : (r & 3)) * 32 + (D == 256 ? (r >> 2 & 1) : 0) * 16 + (r & 1) * 8;
 }
 template <int D>
 __device__ __forceinline__ uint32_t v_at(uint32_t r, uint32_t elem) {
@@ -696,24 +712,29 @@ __device__ __forceinline__ uint32_t v_at(uint32_t r, uint32_t elem) {
 }
 
 template <int D, bool FP8, int WAVES>
-__device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, const Cursor& cur, const Request& q, const Span& s,
+__device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l, const Cursor& cur, const Request& q, const Span& s,
                                           uint32_t k0, uint32_t k1) {
-  constexpr int KT = Lds32<D>::KT, NB = KT / 32, kThreads = 64 * WAVES;
+  constexpr int R = rows_of_wave(D), KT = LdsMany<D>::KT, kThreads = 64 * WAVES;
+  constexpr int NB = KT / R, S = R * R / 64;       // scores: blocks of R keys, and of each so many to a lane
+  constexpr int DB = D / R;                        // output: blocks of R elements, so many to a lane as well
+  constexpr int kParts = 64 / R;                   // lanes of a row
+  constexpr int kDepth = 8 * kParts;               // elements (or keys) of a product
+  typedef Products<R> Mfma;
   constexpr int kRow = FP8 ? D : 2 * D;                    // bytes of a head's row
   constexpr int kPieces = kRow / 16;                       // 16-byte pieces of a key
   constexpr int kKeys = kThreads / kPieces;                // keys that the threads bring at a time
   constexpr int kLoads = KT < kKeys ? 1 : KT / kKeys;      // pieces of K (and of V) per thread
   constexpr int kWaveKeys = 64 / kPieces;                  // keys of a wavefront at a time
-  constexpr uint32_t kBatch = 4, kDs = D == 64 ? 2 : 4;    // products whose operands are read at a time
+  constexpr uint32_t kBatch = 4, kDs = D == 64 ? 2 : 4;  // products whose operands are read at a time
   const Kind& kind = a.kind[1];
-  const uint32_t tid = threadIdx.x, lane = tid & 63, c = lane % 32, half = lane / 32;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, c = lane % R, part = lane / R;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const GlobalBytes kp = layer_base(a.c.k), vp = layer_base(a.c.v);
   const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
   const uint32_t kv = cur.head / kind.parts;
 
-  const uint32_t m = wave * 32 + c;
-  bf16x8 qf[D / 16];
+  const uint32_t m = wave * R + c;
+  bf16x8 qf[D / kDepth];
   int row_lo, row_hi;  // keys that this lane's row sees
   // keys that some row of this wavefront sees, and keys that all of them see
   int wave_lo, wave_hi, all_lo, all_hi;
@@ -721,11 +742,11 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
     const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) qf[k] = load_q(a, qp + k * 16 + half * 8, p.there);
+    for (int k = 0; k < D / kDepth; ++k) qf[k] = load_q(a, qp + k * kDepth + part * 8, p.there);
     row_lo = p.lo;
     row_hi = p.hi;
     int lo = p.there ? p.lo : 0x7fffffff, hi = p.there ? p.hi : 0, lo2 = p.there ? p.lo : 0, hi2 = p.there ? p.hi : 0x7fffffff;
-    for (uint32_t k = 1; k < 32; k *= 2) {
+    for (uint32_t k = 1; k < R; k *= 2) {
       lo = min(lo, __shfl_xor(lo, k));
       hi = max(hi, __shfl_xor(hi, k));
       lo2 = max(lo2, __shfl_xor(lo2, k));
@@ -736,11 +757,11 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     all_lo = uniform(lo2);
     all_hi = uniform(hi2);
   }
-  f32x16 o[D / 32];
+  typename Mfma::Sum o[DB];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
+  for (int i = 0; i < DB; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    for (int j = 0; j < S; ++j) o[i][j] = 0.f;
   Soft st = {kNone, 0.f, 0.f};
 
   const int blocks = (int)(k1 - k0), block0 = (int)(s.b0 + k0) * KT;
@@ -842,17 +863,17 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   // Where this lane finds its part of a product's K and V, in bytes of shared
   // memory. The product's number goes in by an exclusive or, at the read itself:
   // one register each, not one for each product.
-  const uint32_t k_lane = lds_of(l.k[0]) + c * D * 2 + (half ^ (k_swap<D>(c) & 1)) * 16 + k_swap<D>(c) / 2 * 32;
+  const uint32_t k_lane = lds_of(l.k[0]) + c * D * 2 + (part ^ k_swap<D>(c)) * 16;
   auto v_lane = [&]() {
     // the lane's number, asked for at every use: kept, this would be spilled, and
     // waited for together with the loads on their way
     uint32_t i;
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(i));
-    const uint32_t v_row = i / 32 * 4 + i % 16 / 4;
-    return lds_of(l.v[0]) + v_row * D * 2 + ((i / 16 % 2 * 16 + i % 4 * 4) ^ v_swap<D>(v_row)) * 2;
+    const uint32_t v_row = i / R * 4 + i % 16 / 4;
+    return lds_of(l.v[0]) + v_row * D * 2 + ((i % R / 16 * 16 + i % 4 * 4) ^ v_swap<D>(v_row)) * 2;
   };
-  f32x16 x[NB];  // a block's scores
-  bf16x8 w[2 * NB];  // and weights
+  typename Mfma::Sum x[NB];    // a block's scores
+  bf16x8 w[KT / kDepth];       // and weights
 
   auto used = [&](int n) { return block0 + n * KT < wave_hi && block0 + n * KT + KT > wave_lo; };
   // x = K Q^T of block n, the operands read a batch ahead
@@ -862,23 +883,23 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     auto read = [&](uint32_t i) {
 #pragma unroll
       for (uint32_t j = 0; j < kBatch; ++j) {
-        const uint32_t at = i * kBatch + j, b = at / (D / 16), k = at % (D / 16);
-        kf[i & 1][j] = *(LdsU32x4)((LdsAddress)(uintptr_t)(from ^ k * 32) + b * 32 * D * 2);
+        const uint32_t at = i * kBatch + j, b = at / (D / kDepth), k = at % (D / kDepth);
+        kf[i & 1][j] = *(LdsU32x4)((LdsAddress)(uintptr_t)(from ^ k * kDepth * 2) + b * R * D * 2);
       }
     };
     read(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) x[b][j] = 0.f;
+      for (int j = 0; j < S; ++j) x[b][j] = 0.f;
 #pragma unroll
-    for (uint32_t i = 0; i < NB * D / 16 / kBatch; ++i) {
-      if (i + 1 < NB * D / 16 / kBatch) read(i + 1);
+    for (uint32_t i = 0; i < NB * D / kDepth / kBatch; ++i) {
+      if (i + 1 < NB * D / kDepth / kBatch) read(i + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (uint32_t j = 0; j < kBatch; ++j) {
-        const uint32_t at = i * kBatch + j, b = at / (D / 16), k = at % (D / 16);
-        x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(kf[i & 1][j]), qf[k], x[b], 0, 0, 0);
+        const uint32_t at = i * kBatch + j, b = at / (D / kDepth), k = at % (D / kDepth);
+        x[b] = Mfma::add(as_bf16(kf[i & 1][j]), qf[k], x[b]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -887,21 +908,21 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   auto weigh = [&](uint32_t n) {
     const int key0 = block0 + (int)n * KT;
     if (holes || key0 < all_lo || key0 + KT > all_hi) {  // some row may not see some key
-      const int first = key0 + 4 * (int)half;
+      const int first = key0 + 4 * (int)part;
       uint32_t bits = ~0u;
       if (holes)
 #pragma unroll 1
-        for (uint32_t t = 0; t < 16 * NB; ++t) {
-          const int key = first + (int)(t / 4 * 8 + t % 4);
+        for (uint32_t t = 0; t < S * NB; ++t) {
+          const int key = first + (int)(t / S * R + t % S / 4 * 8 + t % 4);
           const bool in = key >= row_lo && key < row_hi;
           if (!in || (uint32_t)table[a.b.page.div((uint32_t)key)] >= a.c.n_pages) bits &= ~(1u << t);
         }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int key = first + 32 * b + 8 * (j / 4) + j % 4;
-          const bool there = (bits >> (16 * b + j) & 1) && key >= row_lo && key < row_hi;
+        for (int j = 0; j < S; ++j) {
+          const int key = first + R * b + 8 * (j / 4) + j % 4;
+          const bool there = (bits >> (S * b + j) & 1) && key >= row_lo && key < row_hi;
           x[b][j] = there ? x[b][j] : kNone;
         }
     }
@@ -909,9 +930,10 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) top = fmaxf(top, x[b][j]);
+      for (int j = 0; j < S; ++j) top = fmaxf(top, x[b][j]);
     top *= a.scale;
     if (__any(top > st.m + kSlack)) {
+      if constexpr (R == 16) top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float mm = fmaxf(st.m, top);
       const float now = mm == kNone ? 0.f : mm;
@@ -920,31 +942,31 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
       st.top = now;
       st.sum *= by;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) o[i] *= by;
+      for (int i = 0; i < DB; ++i) o[i] *= by;
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
+      for (int j = 0; j < S; ++j) {
         const float y = exp2_(__builtin_fmaf(x[b][j], a.scale, -st.top));
         st.sum += y;
-        w[2 * b + j / 8][j % 8] = (__bf16)y;
+        w[(S * b + j) / 8][(S * b + j) % 8] = (__bf16)y;
       }
   };
   // o += V^T w of block n, the operands read a batch ahead
   auto values = [&](uint32_t n) {
     const uint32_t from = v_lane() + (n & 1) * KT * D * 2;
-    constexpr uint32_t kSteps = 2 * NB * (D / 32) / kDs;
+    constexpr uint32_t kSteps = KT / kDepth * DB / kDs;
     u32x2 vf[2][2 * kDs];
     auto read = [&](uint32_t i) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s16x4* Lds4;
 #pragma unroll
       for (uint32_t j = 0; j < kDs; ++j) {
-        const uint32_t t = i / (D / 32 / kDs), d = i % (D / 32 / kDs) * kDs + j;
-        const LdsAddress v = (LdsAddress)(uintptr_t)(from ^ d * 64) + t * 16 * D * 2;
+        const uint32_t t = i / (DB / kDs), d = i % (DB / kDs) * kDs + j;
+        const LdsAddress v = (LdsAddress)(uintptr_t)(from ^ d * R * 2) + t * kDepth * D * 2;
         vf[i & 1][2 * j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)v));
-        vf[i & 1][2 * j + 1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(v + 8 * D * 2)));
+        vf[i & 1][2 * j + 1] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4)(v + kDepth / 2 * D * 2)));
       }
     };
     read(0);
@@ -954,9 +976,9 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (uint32_t j = 0; j < kDs; ++j) {
-        const uint32_t t = i / (D / 32 / kDs), d = i % (D / 32 / kDs) * kDs + j;
+        const uint32_t t = i / (DB / kDs), d = i % (DB / kDs) * kDs + j;
         const u32x2 lo = vf[i & 1][2 * j], hi = vf[i & 1][2 * j + 1];
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]}), w[t], o[d], 0, 0, 0);
+        o[d] = Mfma::add(as_bf16(u32x4{lo[0], lo[1], hi[0], hi[1]}), w[t], o[d]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -1028,7 +1050,9 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     }
   }
 
-  const float sum = st.sum + __shfl_xor(st.sum, 32);
+  float sum = st.sum;
+  if constexpr (R == 16) sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
   const bool whole = k0 == 0 && k1 == s.n;
   const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
   if (p.there) {
@@ -1037,16 +1061,16 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
     uint16_t* op = a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head;
     float* fp = a.part_o + (slot + m) * D;
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        const uint32_t at = d * 32 + 2 * j + 4 * half;
+      for (int j = 0; j < S; j += 4) {
+        const uint32_t at = d * R + 2 * j + 4 * part;
         if (whole)
           store_bf16x4(op + at, o[d][j] * inv, o[d][j + 1] * inv, o[d][j + 2] * inv, o[d][j + 3] * inv);
         else
           *(f32x4*)(fp + at) = f32x4{o[d][j], o[d][j + 1], o[d][j + 2], o[d][j + 3]};
       }
-    if (half == 0) {
+    if (part == 0) {
       if (!whole)
         *(f32x2*)(a.part_ml + (slot + m) * 2) = f32x2{st.m, sum};
       else if (a.lse)
@@ -1055,13 +1079,14 @@ __device__ __forceinline__ void segment32(const AttendArgs& a, Lds32<D>& l, cons
   }
 }
 
-// Tiles of 32 rows for each wavefront, and of 16 for requests of few rows.
+// Tiles of many rows, and of 16 for requests of few (heads of 256: their 16-row
+// tiles want the registers of one wavefront on a SIMD, and stay in k_attend16).
 template <int D, bool FP8, bool EVEN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend32(AttendArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
   __shared__ union {
     PlanLds plan;
-    Lds16<D, WAVES> few;
-    Lds32<D> many;
+    Lds16<D, D == 256 ? 1 : WAVES> few;
+    LdsMany<D> many;
   } l;
   Cursor cur;
   const bool any = plan(a, l.plan, cur);
@@ -1074,9 +1099,9 @@ __global__ __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) void k_attend32(Atten
     const Span s = span_of(a, q, cur.tile);
     const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s);
-    if (q.kind)
-      segment32<D, FP8, WAVES>(a, l.many, cur, q, s, k0, k1);
-    else
+    if (D == 256 || q.kind)
+      segment_many<D, FP8, WAVES>(a, l.many, cur, q, s, k0, k1);
+    else if constexpr (D != 256)
       segment16<D, FP8, EVEN, WAVES>(a, l.few, cur, q, s, k0, k1);
     cur.at = cur.first + k1;
     if (k1 == s.n) {
@@ -1169,7 +1194,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 
 // ---- launching ----------------------------------------------------------------------------
 struct Shape {
-  uint32_t waves;      // of a workgroup; 0: k_attend16, else k_attend32 with so many
+  uint32_t waves;      // of a workgroup; 0: k_attend16, else k_attend_many with so many
   uint32_t workers;    // workgroups: as many as the device holds at a time
   uint32_t slot_rows;
   Kind kind[2];
@@ -1189,9 +1214,9 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   Shape s;
   const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
   const uint64_t per = n_rows * group / (n_reqs ? n_reqs : 1);
-  s.waves = per <= 32 ? 0 : ctx->D == 256 || per <= 128 ? 4 : 8;
+  s.waves = per <= 32 ? 0 : ctx->D == 256 || per > 128 ? 8 : 4;
   s.workers = ctx->D == 256 || s.waves == 8 ? 256 : 512;
-  s.few = s.waves ? 32 / group : ~0u;
+  s.few = !s.waves ? ~0u : ctx->D == 256 ? 0 : 32 / group;
   Kind& f = s.kind[0];
   f = kind_of(ctx, group, 16);
   const uint32_t runs = ctx->H * f.parts;
@@ -1201,10 +1226,10 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   // keys of a wavefront's step, and how many wavefronts take steps of one run
   f.block_shift = (ctx->D * wide < 128 ? 6 : 5) + (s.waves == 8 ? 3 : 2) - f.heads_shift;
   Kind& m = s.kind[1];
-  m = kind_of(ctx, group, 32 * (s.waves ? s.waves : 4));
+  m = kind_of(ctx, group, rows_of_wave(ctx->D) * (s.waves ? s.waves : 4));
   m.heads_shift = 0;
   m.heads = ctx->H * m.parts;
-  m.block_shift = ctx->D == 256 ? 5 : 6;
+  m.block_shift = 6;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
   return s;
@@ -1229,10 +1254,10 @@ void launch(const Shape& sh, hipStream_t s, const AttendArgs& a) {
     const dim3 grid(sh.workers);
     if (!sh.waves)
       hipLaunchKernelGGL((k_attend16<D, FP8, EVEN>), grid, dim3(256), 0, s, a);
-    else if (sh.waves == 4)
-      hipLaunchKernelGGL((k_attend32<D, FP8, EVEN, 4>), grid, dim3(256), 0, s, a);
+    else if (sh.waves == 8)
+      hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 8>), grid, dim3(512), 0, s, a);
     else if constexpr (D != 256)
-      hipLaunchKernelGGL((k_attend32<D, FP8, EVEN, 8>), grid, dim3(512), 0, s, a);
+      hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 4>), grid, dim3(256), 0, s, a);
   }
   TimedLaunch timed(TL_KERNEL_ATTEND_JOIN, s);
   hipLaunchKernelGGL((k_attend_join<D>), dim3((sh.workers - 1) * (a.slot_rows * D / 1024)), dim3(256), 0, s, a);
