@@ -24,6 +24,10 @@ struct Share {
   uint32_t row0, rows;  // of the request
 };
 
+// Not a generic pointer: with such a store on its way, every wait for a load is
+// for all of them.
+typedef __attribute__((address_space(1))) Share* GlobalShare;
+
 // How requests are cut into tiles: of 16 rows, or of 32 for each wavefront.
 struct Kind {
   uint32_t rows;               // of a tile
@@ -32,6 +36,7 @@ struct Kind {
   uint32_t heads_shift;        // log2 of the runs that a workgroup takes together
   uint32_t heads;              // how many times it does so for a batch row's heads
   uint32_t block_shift;        // log2 of the keys of a block
+  uint32_t cost;               // what a tile takes besides its blocks, in blocks: finding it, its queries, its result
 };
 
 struct AttendArgs {
@@ -64,7 +69,7 @@ constexpr float kSlack = 8.f;  // how far a block's scores may exceed the runnin
 struct Request {
   uint32_t row0, rows, tiles;
   int held, before;  // keys, and keys before the first row's own
-  uint32_t kind, tile_rows, heads, block_shift;  // as in Kind
+  uint32_t kind, tile_rows, heads, block_shift, cost;  // as in Kind
 };
 
 __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
@@ -78,6 +83,7 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
   q.tile_rows = q.kind ? a.kind[1].tile_rows : a.kind[0].tile_rows;
   q.heads = q.kind ? a.kind[1].heads : a.kind[0].heads;
   q.block_shift = q.kind ? a.kind[1].block_shift : a.kind[0].block_shift;
+  q.cost = q.kind ? a.kind[1].cost : a.kind[0].cost;
   q.tiles = (q.rows + q.tile_rows - 1) / q.tile_rows;
   return q;
 }
@@ -90,7 +96,7 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 }
 __device__ __forceinline__ Request uniform(Request q) {
   return Request{uniform(q.row0), uniform(q.rows), uniform(q.tiles), uniform(q.held), uniform(q.before),
-                 uniform(q.kind), uniform(q.tile_rows), uniform(q.heads), uniform(q.block_shift)};
+                 uniform(q.kind), uniform(q.tile_rows), uniform(q.heads), uniform(q.block_shift), uniform(q.cost)};
 }
 
 struct Span {
@@ -114,16 +120,16 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, u
   return s;
 }
 
-// Blocks of a request's tiles tile0, tile0 + step, ...
-__device__ __forceinline__ uint64_t blocks_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
+// Units of a request's tiles tile0, tile0 + step, ...
+__device__ __forceinline__ uint64_t units_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
   uint64_t n = 0;
-  for (uint32_t t = tile0; t < q.tiles; t += step) n += span_of(a, q, t).n;
+  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + span_of(a, q, t).n;
   return n;
 }
 
 // ---- work ------------------------------------------------------------------------
 // Units of work are numbered: requests in order, a request's heads, a head's
-// tiles, a tile's blocks of keys. A worker (a workgroup) takes an equal run of
+// tiles, a tile's cost and its blocks of keys. A worker (a workgroup) takes an equal run of
 // them, which it works out from the lengths on the device: requests of any
 // lengths keep all workers busy to the end. A tile whose blocks fall to several
 // workers is put together by k_attend_join.
@@ -151,12 +157,12 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   if (split > 1) {
     if (tid / split < n) {
       const Request q = request_of(a, tid / split);
-      mine = blocks_of(a, q, tid % split, split) * q.heads;
+      mine = units_of(a, q, tid % split, split) * q.heads;
     }
   } else if (tid < kPlan) {
     for (uint32_t r = tid * per; r < min(tid * per + per, n); ++r) {
       const Request q = request_of(a, r);
-      mine += blocks_of(a, q, 0, 1) * q.heads;
+      mine += units_of(a, q, 0, 1) * q.heads;
     }
   }
   uint64_t incl = mine;
@@ -195,19 +201,19 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   c.first = uniform(l.found_at);
   while (c.r < n) {
     const Request q = uniform(request_of(a, c.r));
-    const uint64_t blocks = split > 1 ? uniform(l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : blocks_of(a, q, 0, 1);
-    if (c.at < c.first + blocks * q.heads) {
-      c.head = (uint32_t)((c.at - c.first) / blocks);
-      c.first += c.head * blocks;
+    const uint64_t units = split > 1 ? uniform(l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : units_of(a, q, 0, 1);
+    if (c.at < c.first + units * q.heads) {
+      c.head = (uint32_t)((c.at - c.first) / units);
+      c.first += c.head * units;
       c.tile = 0;
       for (;;) {
-        const uint32_t k = span_of(a, q, c.tile).n;
+        const uint32_t k = q.cost + span_of(a, q, c.tile).n;
         if (c.at < c.first + k) return true;
         c.first += k;
         ++c.tile;
       }
     }
-    c.first += blocks * q.heads;
+    c.first += units * q.heads;
     ++c.r;
   }
   return false;
@@ -227,10 +233,14 @@ __device__ __forceinline__ void next_tile(const AttendArgs& a, const Request& q,
 // floor(total * w / workers). The second worker of a tile sees to it.
 __device__ void note_share(const AttendArgs& a, const Cursor& c, const Request& q, const Span& s) {
   Share sh = {0, q.kind, c.head, c.tile, q.row0, q.rows};
-  const uint64_t end = c.first + s.n;
-  if (c.at > c.first && c.total * (c.worker - 1) < (c.first + 1) * c.workers)
+  const uint64_t block0 = c.first + q.cost, end = block0 + s.n;
+  if (c.at > block0 && c.total * (c.worker - 1) < (block0 + 1) * c.workers)
     sh.parts = (uint32_t)((end * c.workers - 1) / c.total) + 2 - c.worker;
-  a.share[c.worker] = sh;
+  typedef __attribute__((address_space(1))) u32x2* Out;
+  const Out to = (Out)(a.share + c.worker);
+  to[0] = u32x2{sh.parts, sh.kind};
+  to[1] = u32x2{sh.head, sh.tile};
+  to[2] = u32x2{sh.row0, sh.rows};
 }
 
 // ---- one row ------------------------------------------------------------------------
@@ -547,18 +557,27 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     const int mine = (int)(lane & (Tile::kKeys - 1));
     auto edge = [&](int key) { return key + Tile::kKeys > first_hi || key < last_lo; };
     Tile ta, tb;
-    Ids16 id = ids16<EVEN>(a, table, key0 + mine, s);
+    // Page ids are asked for two steps ahead and before the keys of the step
+    // between: who waits for them does not wait for those.
+    // Past the last step there are no keys to find: the same row is read, from near.
+    auto ids = [&](int key) { return ids16<EVEN>(a, table, key <= last ? key + mine : 0x7fffff00, s); };
+    Ids16 id = ids(key0), later = ids(key0 + step);
     load16<D, FP8, EVEN>(a, kp, vp, kv, id, ta);
-    id = ids16<EVEN>(a, table, min(key0 + step, last) + mine, s);
-    for (int key = key0; key <= last; key += 2 * step) {
-      load16<D, FP8, EVEN>(a, kp, vp, kv, id, tb);
-      id = ids16<EVEN>(a, table, min(key + 2 * step, last) + mine, s);
+    auto next = [&](int key, Tile& t) {  // the step from `key` on is on its way, into t
+      id = later;
+      later = ids(key + step);
+      __builtin_amdgcn_sched_barrier(0);
+      load16<D, FP8, EVEN>(a, kp, vp, kv, id, t);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int key = key0;
+    for (; key + step <= last; key += 2 * step) {  // no way out in between: it would have every load waited for
+      next(key + step, tb);
       block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), r);
-      if (key + step > last) break;
-      load16<D, FP8, EVEN>(a, kp, vp, kv, id, ta);
-      id = ids16<EVEN>(a, table, min(key + 3 * step, last) + mine, s);
+      next(key + 2 * step, ta);
       block16<D, FP8, EVEN>(a, tb, kv, key + step, p, edge(key + step), r);
     }
+    if (key <= last) block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), r);
   }
 
   float sum = r.s.sum;
@@ -635,18 +654,22 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a
   Cursor cur;
   const bool any = plan(a, l.plan, cur);
   if (!any) {
-    if (threadIdx.x == 0) a.share[cur.worker].parts = 0;
+    if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
   for (bool first = true; cur.at < cur.end; first = false) {
     const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
-    const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
+    // the worker's blocks of this tile: none where its run ends within the tile's cost
+    const uint64_t block0 = cur.first + q.cost;
+    const uint32_t k0 = cur.at > block0 ? (uint32_t)(cur.at - block0) : 0;
+    const uint32_t k1 = cur.end > block0 ? (uint32_t)min((uint64_t)s.n, cur.end - block0) : 0;
     if (first && threadIdx.x == 0) note_share(a, cur, q, s);
+    if (k1 == 0) break;
     segment16<D, FP8, EVEN, 4>(a, l.s, cur, q, s, k0, k1);
-    cur.at = cur.first + k1;
+    cur.at = min(cur.end, block0 + s.n);
     if (k1 == s.n) {
-      cur.first += s.n;
+      cur.first = block0 + s.n;
       if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
@@ -1091,21 +1114,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
   Cursor cur;
   const bool any = plan(a, l.plan, cur);
   if (!any) {
-    if (threadIdx.x == 0) a.share[cur.worker].parts = 0;
+    if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
   for (bool first = true; cur.at < cur.end; first = false) {
     const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
-    const uint32_t k0 = (uint32_t)(cur.at - cur.first), k1 = (uint32_t)min((uint64_t)s.n, cur.end - cur.first);
+    // the worker's blocks of this tile: none where its run ends within the tile's cost
+    const uint64_t block0 = cur.first + q.cost;
+    const uint32_t k0 = cur.at > block0 ? (uint32_t)(cur.at - block0) : 0;
+    const uint32_t k1 = cur.end > block0 ? (uint32_t)min((uint64_t)s.n, cur.end - block0) : 0;
     if (first && threadIdx.x == 0) note_share(a, cur, q, s);
+    if (k1 == 0) break;
     if (D == 256 || q.kind)
       segment_many<D, FP8, WAVES>(a, l.many, cur, q, s, k0, k1);
     else if constexpr (D != 256)
       segment16<D, FP8, EVEN, WAVES>(a, l.few, cur, q, s, k0, k1);
-    cur.at = cur.first + k1;
+    cur.at = min(cur.end, block0 + s.n);
     if (k1 == s.n) {
-      cur.first += s.n;
+      cur.first = block0 + s.n;
       if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
@@ -1119,7 +1146,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
 template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   constexpr uint32_t kLanes = D / 4, kRuns = 256 / kLanes;
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 8;  // parts on their way at a time
   __shared__ struct {
     float top[kRuns], sum[kRuns];
     f32x4 y[kRuns][kLanes];
@@ -1225,11 +1252,13 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   f.heads = runs >> f.heads_shift;
   // keys of a wavefront's step, and how many wavefronts take steps of one run
   f.block_shift = (ctx->D * wide < 128 ? 6 : 5) + (s.waves == 8 ? 3 : 2) - f.heads_shift;
+  f.cost = 1;
   Kind& m = s.kind[1];
   m = kind_of(ctx, group, rows_of_wave(ctx->D) * (s.waves ? s.waves : 4));
   m.heads_shift = 0;
   m.heads = ctx->H * m.parts;
   m.block_shift = 6;
+  m.cost = 4;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
   return s;
