@@ -36,7 +36,8 @@ struct Kind {
   uint32_t heads_shift;        // log2 of the runs that a workgroup takes together
   uint32_t heads;              // how many times it does so for a batch row's heads
   uint32_t block_shift;        // log2 of the keys of a block
-  uint32_t cost;               // what a tile takes besides its blocks, in blocks: finding it, its queries, its result
+  uint32_t weight;             // units of a block
+  uint32_t cost;               // units that a tile takes besides: finding it, its queries, its result
 };
 
 struct AttendArgs {
@@ -69,7 +70,7 @@ constexpr float kSlack = 8.f;  // how far a block's scores may exceed the runnin
 struct Request {
   uint32_t row0, rows, tiles;
   int held, before;  // keys, and keys before the first row's own
-  uint32_t kind, tile_rows, heads, block_shift, cost;  // as in Kind
+  uint32_t kind, tile_rows, heads, block_shift, weight, cost;  // as in Kind
 };
 
 __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
@@ -83,6 +84,7 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
   q.tile_rows = q.kind ? a.kind[1].tile_rows : a.kind[0].tile_rows;
   q.heads = q.kind ? a.kind[1].heads : a.kind[0].heads;
   q.block_shift = q.kind ? a.kind[1].block_shift : a.kind[0].block_shift;
+  q.weight = q.kind ? a.kind[1].weight : a.kind[0].weight;
   q.cost = q.kind ? a.kind[1].cost : a.kind[0].cost;
   q.tiles = (q.rows + q.tile_rows - 1) / q.tile_rows;
   return q;
@@ -96,7 +98,7 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 }
 __device__ __forceinline__ Request uniform(Request q) {
   return Request{uniform(q.row0), uniform(q.rows), uniform(q.tiles), uniform(q.held), uniform(q.before),
-                 uniform(q.kind), uniform(q.tile_rows), uniform(q.heads), uniform(q.block_shift), uniform(q.cost)};
+                 uniform(q.kind), uniform(q.tile_rows), uniform(q.heads), uniform(q.block_shift), uniform(q.weight), uniform(q.cost)};
 }
 
 struct Span {
@@ -123,7 +125,7 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, u
 // Units of a request's tiles tile0, tile0 + step, ...
 __device__ __forceinline__ uint64_t units_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
   uint64_t n = 0;
-  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + span_of(a, q, t).n;
+  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + q.weight * span_of(a, q, t).n;
   return n;
 }
 
@@ -182,7 +184,7 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   if (tid == 0) l.found = ~0u;
   __syncthreads();
   c.total = uniform(l.sum[kPlan]);
-  c.workers = (uint32_t)min((uint64_t)gridDim.x, c.total);
+  c.workers = (uint32_t)min((uint64_t)gridDim.x, (c.total + a.kind[1].weight - 1) / a.kind[1].weight);  // a block for each, at least
   // runs that follow each other go to workgroups of one chiplet, which share an L2
   c.worker = blockIdx.x;
   if (c.workers == gridDim.x && gridDim.x % 8 == 0) c.worker = c.worker % 8 * (gridDim.x / 8) + c.worker / 8;
@@ -207,7 +209,7 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
       c.first += c.head * units;
       c.tile = 0;
       for (;;) {
-        const uint32_t k = q.cost + span_of(a, q, c.tile).n;
+        const uint32_t k = q.cost + q.weight * span_of(a, q, c.tile).n;
         if (c.at < c.first + k) return true;
         c.first += k;
         ++c.tile;
@@ -219,23 +221,35 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   return false;
 }
 
+// The blocks [k0, k1) of the cursor's tile that begin in its run (none where the run
+// ends within the tile's cost, or begins within its last block), and the tile's end.
+__device__ __forceinline__ uint64_t blocks_of(const Cursor& c, const Request& q, const Span& s, uint32_t& k0, uint32_t& k1) {
+  const int64_t n = (int64_t)s.n * q.weight;
+  const uint64_t block0 = c.first + q.cost;
+  const uint32_t u0 = (uint32_t)min(n, max((int64_t)0, (int64_t)(c.at - block0)));
+  const uint32_t u1 = (uint32_t)min(n, max((int64_t)0, (int64_t)(c.end - block0)));
+  k0 = (u0 + q.weight - 1) / q.weight;
+  k1 = (u1 + q.weight - 1) / q.weight;
+  return block0 + n;
+}
+
 // The tile after the cursor's; its first unit is c.first.
-__device__ __forceinline__ void next_tile(const AttendArgs& a, const Request& q, Cursor& c) {
+__device__ __forceinline__ void next_tile(const AttendArgs& a, Request& q, Cursor& c) {
   if (++c.tile < q.tiles) return;
   c.tile = 0;
   if (++c.head < q.heads) return;
   c.head = 0;
-  while (++c.r < a.b.n_reqs && request_of(a, c.r).tiles == 0) {
+  while (++c.r < a.b.n_reqs && (q = uniform(request_of(a, c.r))).tiles == 0) {
   }
 }
 
 // A worker's first tile, for the joining kernel: worker w's run begins at
 // floor(total * w / workers). The second worker of a tile sees to it.
-__device__ void note_share(const AttendArgs& a, const Cursor& c, const Request& q, const Span& s) {
+__device__ void note_share(const AttendArgs& a, const Cursor& c, const Request& q, const Span& s, uint32_t k0, uint32_t k1) {
   Share sh = {0, q.kind, c.head, c.tile, q.row0, q.rows};
-  const uint64_t block0 = c.first + q.cost, end = block0 + s.n;
-  if (c.at > block0 && c.total * (c.worker - 1) < (block0 + 1) * c.workers)
-    sh.parts = (uint32_t)((end * c.workers - 1) / c.total) + 2 - c.worker;
+  const uint64_t block0 = c.first + q.cost, last = block0 + (uint64_t)(s.n - 1) * q.weight;  // where its first and last block begin
+  if (k0 > 0 && k0 < k1 && c.total * (c.worker - 1) < (block0 + 1) * c.workers)  // this worker goes on with it, the one before begins it
+    sh.parts = (uint32_t)(((last + 1) * c.workers - 1) / c.total) + 2 - c.worker;
   typedef __attribute__((address_space(1))) u32x2* Out;
   const Out to = (Out)(a.share + c.worker);
   to[0] = u32x2{sh.parts, sh.kind};
@@ -657,19 +671,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a
     if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
+  Request q = uniform(request_of(a, cur.r));
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
-    // the worker's blocks of this tile: none where its run ends within the tile's cost
-    const uint64_t block0 = cur.first + q.cost;
-    const uint32_t k0 = cur.at > block0 ? (uint32_t)(cur.at - block0) : 0;
-    const uint32_t k1 = cur.end > block0 ? (uint32_t)min((uint64_t)s.n, cur.end - block0) : 0;
-    if (first && threadIdx.x == 0) note_share(a, cur, q, s);
-    if (k1 == 0) break;
-    segment16<D, FP8, EVEN, 4>(a, l.s, cur, q, s, k0, k1);
-    cur.at = min(cur.end, block0 + s.n);
-    if (k1 == s.n) {
-      cur.first = block0 + s.n;
+    uint32_t k0, k1;
+    const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
+    if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
+    if (k0 < k1) segment16<D, FP8, EVEN, 4>(a, l.s, cur, q, s, k0, k1);
+    cur.at = min(cur.end, tile_end);
+    if (cur.at == tile_end) {
+      cur.first = tile_end;
       if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
@@ -759,8 +770,6 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   const uint32_t m = wave * R + c;
   bf16x8 qf[D / kDepth];
   int row_lo, row_hi;  // keys that this lane's row sees
-  // keys that some row of this wavefront sees, and keys that all of them see
-  int wave_lo, wave_hi, all_lo, all_hi;
   {
     const Place p = place_of(a, kind, q, cur.head, cur.tile, m);
     const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
@@ -768,17 +777,21 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
     for (int k = 0; k < D / kDepth; ++k) qf[k] = load_q(a, qp + k * kDepth + part * 8, p.there);
     row_lo = p.lo;
     row_hi = p.hi;
-    int lo = p.there ? p.lo : 0x7fffffff, hi = p.there ? p.hi : 0, lo2 = p.there ? p.lo : 0, hi2 = p.there ? p.hi : 0x7fffffff;
-    for (uint32_t k = 1; k < R; k *= 2) {
-      lo = min(lo, __shfl_xor(lo, k));
-      hi = max(hi, __shfl_xor(hi, k));
-      lo2 = max(lo2, __shfl_xor(lo2, k));
-      hi2 = min(hi2, __shfl_xor(hi2, k));
+  }
+  // keys that some row of this wavefront sees, and keys that all of them see: its
+  // first token's and its last's
+  int wave_lo = 0x7fffffff, wave_hi = 0, all_lo = 0, all_hi = 0x7fffffff;
+  {
+    const uint32_t tokens = min(kind.tile_rows, q.rows - cur.tile * kind.tile_rows);
+    const uint32_t t0 = wave * R / kind.part_heads, t1 = min((wave * R + R - 1) / kind.part_heads, tokens - 1);
+    if (t0 < tokens) {
+      const Place p0 = place_of(a, kind, q, cur.head, cur.tile, t0 * kind.part_heads);
+      const Place p1 = place_of(a, kind, q, cur.head, cur.tile, t1 * kind.part_heads);
+      wave_lo = uniform(p0.lo);
+      wave_hi = uniform(p1.hi);
+      all_lo = uniform(p1.lo);
+      all_hi = uniform(p0.hi);
     }
-    wave_lo = uniform(lo);
-    wave_hi = uniform(hi);
-    all_lo = uniform(lo2);
-    all_hi = uniform(hi2);
   }
   typename Mfma::Sum o[DB];
 #pragma unroll
@@ -789,14 +802,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
 
   const int blocks = (int)(k1 - k0), block0 = (int)(s.b0 + k0) * KT;
   const uint32_t step = a.n_heads * kRow;  // bytes from a key to the next
-  // whether a page of these blocks is missing (rare: then every key is asked)
-  bool holes = false;
-  if (s.hi > s.lo) {
-    const uint32_t first = a.b.page.div((uint32_t)max(s.lo, block0)), last = a.b.page.div((uint32_t)min(s.hi, block0 + blocks * KT) - 1);
-    int gone = 0;
-    for (uint32_t i = first + tid; i <= last; i += kThreads) gone |= (uint32_t)table[i] >= a.c.n_pages;
-    holes = __syncthreads_or(gone);
-  }
+  bool holes = false;  // whether a page of these blocks is missing (rare: then every key is asked)
   // What a thread brings: a 16-byte piece of K and V of kLoads keys of a block.
   // Keys that no row sees are read from the nearest one that some row does.
   const uint32_t piece = lane / kWaveKeys, my_key = wave * kWaveKeys + lane % kWaveKeys;
@@ -1010,10 +1016,15 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   if (s.hi > s.lo) {
     // Block n is kept in buffers n % 2. Past the last block its last key is read
     // again. Page ids are looked up a step before they are used.
-    __syncthreads();
     find(0);
+    int gone = 0;
+    {
+      const uint32_t first = a.b.page.div((uint32_t)max(s.lo, block0)), end = a.b.page.div((uint32_t)min(s.hi, block0 + blocks * KT) - 1);
+      for (uint32_t i = first + tid; i <= end; i += kThreads) gone |= (uint32_t)table[i] >= a.c.n_pages;
+    }
     fetch_k();
     find(1);
+    holes = __syncthreads_or(gone);
     if constexpr (WAVES == 8) {
       // Wavefronts 0 to 3 are a phase ahead. A step of theirs keeps K of the next
       // block and V of this one; the others', a phase later, those of the block
@@ -1117,22 +1128,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
     if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
+  Request q = uniform(request_of(a, cur.r));
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Request q = uniform(request_of(a, cur.r));
     const Span s = span_of(a, q, cur.tile);
-    // the worker's blocks of this tile: none where its run ends within the tile's cost
-    const uint64_t block0 = cur.first + q.cost;
-    const uint32_t k0 = cur.at > block0 ? (uint32_t)(cur.at - block0) : 0;
-    const uint32_t k1 = cur.end > block0 ? (uint32_t)min((uint64_t)s.n, cur.end - block0) : 0;
-    if (first && threadIdx.x == 0) note_share(a, cur, q, s);
-    if (k1 == 0) break;
-    if (D == 256 || q.kind)
+    uint32_t k0, k1;
+    const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
+    if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
+    if (k0 == k1) {
+      // none
+    } else if (D == 256 || q.kind) {
       segment_many<D, FP8, WAVES>(a, l.many, cur, q, s, k0, k1);
-    else if constexpr (D != 256)
+    } else if constexpr (D != 256) {
       segment16<D, FP8, EVEN, WAVES>(a, l.few, cur, q, s, k0, k1);
-    cur.at = min(cur.end, block0 + s.n);
-    if (k1 == s.n) {
-      cur.first = block0 + s.n;
+    }
+    cur.at = min(cur.end, tile_end);
+    if (cur.at == tile_end) {
+      cur.first = tile_end;
       if (cur.at < cur.end) next_tile(a, q, cur);
     }
   }
@@ -1252,13 +1263,16 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   f.heads = runs >> f.heads_shift;
   // keys of a wavefront's step, and how many wavefronts take steps of one run
   f.block_shift = (ctx->D * wide < 128 ? 6 : 5) + (s.waves == 8 ? 3 : 2) - f.heads_shift;
-  f.cost = 1;
+  // A block of many rows takes about 1.5 times as long as one of few.
+  f.weight = s.waves ? 2 : 1;
+  f.cost = f.weight;
   Kind& m = s.kind[1];
   m = kind_of(ctx, group, rows_of_wave(ctx->D) * (s.waves ? s.waves : 4));
   m.heads_shift = 0;
   m.heads = ctx->H * m.parts;
   m.block_shift = 6;
-  m.cost = 4;
+  m.weight = s.waves ? 3 : 1;
+  m.cost = 4 * m.weight;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
   return s;
