@@ -361,3 +361,47 @@ class FileRestore:
                     self.file.read(ids[nlo:nhi], self.bufs[k ^ 1])
             self.stream.synchronize()
         return verd[:n]
+
+
+class NewTokens:
+    """The step after a restore: the new tokens of a batch of requests (what a
+    prompt has left behind its restored blocks, or one token of each request in
+    decode) on the engine's paged cache, a layer at a time as the model reaches
+    it. layer() appends the tokens' K and V to their requests' pages, rotated,
+    and returns their queries' attention over everything the pages then hold.
+
+    Device arrays: d_row_off u32 [n + 1] (request i has rows d_row_off[i] ..
+    d_row_off[i + 1] - 1), d_kv_len u32 [n] (tokens of each request, the new ones
+    included), d_tables i32 [n_groups, n, width] (each request's pages in order:
+    the restored ones, then fresh ones), d_cos_sin f32 [positions, rot / 2, 2] or
+    None for keys and queries that are not rotated. One workspace serves all
+    layers; `status` has layer()'s verdict per row (valid after the stream syncs)."""
+
+    def __init__(self, ctx: T.Ctx, cache: PagedCache, n_q_heads: int, n_rows: int, d_row_off, d_kv_len, d_tables,
+                 d_cos_sin=None, stream=None):
+        self.ctx, self.n_rows, self.n_q_heads = ctx, n_rows, n_q_heads
+        self.stream = stream or torch.cuda.current_stream()
+        n, width = d_kv_len.shape[0], d_tables.shape[-1]
+        self.cache, self._pages = cache.tl(), cache
+        self.batch = T.make_batch(n, n_rows, d_row_off, d_kv_len, d_tables, width)
+        self.rope = None if d_cos_sin is None else T.make_rope(d_cos_sin, 2 * d_cos_sin.shape[1])
+        dev = cache.k[0].device
+        with _on(self.stream):
+            self.ws_bytes = T.tl_attend_workspace_bytes(ctx, n_q_heads, n, n_rows)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=dev)
+            self.status = torch.empty(n_rows, dtype=torch.uint8, device=dev)
+            self.q = torch.empty((n_rows, n_q_heads, ctx.head_dim), dtype=torch.bfloat16, device=dev)
+
+    def layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor = None) -> torch.Tensor:
+        """q [n_rows, n_q_heads, D], k and v [n_rows, n_kv_heads, D] in bf16, as
+        the model's projections left them (slices of one tensor will do). Returns
+        [n_rows, n_q_heads, D]."""
+        s = self.stream
+        if s != torch.cuda.current_stream():
+            for x in (q, k, v) + (() if lse is None else (lse,)):
+                x.record_stream(s)  # the caller may drop them before the stream has read them
+        with _on(s):
+            out = torch.empty_like(self.q)
+            T.tl_append(self.ctx, s, l, self.batch, self.cache, k, v, self.rope, q, self.q, self.status)
+            T.tl_attend(self.ctx, s, l, self.batch, self.cache, self.q, out, self.ws, self.ws_bytes, lse=lse)
+        return out
