@@ -567,8 +567,8 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
  * left out, and what a page holds past the request's keys is not used. A row
  * that sees no key gets zeros. d_lse (device [n_rows][n_q_heads] floats, or
  * NULL) gets log(sum_j w_j), minus infinity for such a row.
- * A value that is NaN or infinite may reach every row of a call that shares its
- * request, not only those that see it.
+ * Keys and values that are NaN or infinite reach the rows that see them, and no
+ * others.
  * Two kernels, no memset and no allocation. d_workspace: device, 16-byte
  * aligned, tl_attend_workspace_bytes(...) of it; needs no initialisation, and
  * calls that overlap need separate ones. out must not overlap q. */

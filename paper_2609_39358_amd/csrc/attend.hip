@@ -316,6 +316,69 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
   return sum == 0.f ? kNone : (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
+// ---- values that are not finite ---------------------------------------------------------
+// A row's weight for a key that it does not see is 0, but 0 times NaN is NaN: a
+// value that is not finite would reach the rows of its tile that do not see it. In
+// the blocks whose keys not all rows of a tile see, such values are taken out, and
+// added at the tile's end to the rows that do see them.
+//
+// All bits of the elements of a word that are not finite.
+template <bool FP8>
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
+  if (FP8) return (((w & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+  return (((w >> 7 & 0x00ff00ffu) + 0x00010001u) >> 8 & 0x00010001u) * 0xffffu;
+}
+
+// Four neighbouring elements, 0 in place of finite ones.
+template <bool FP8>
+__device__ __forceinline__ f32x4 odd4(GlobalBytes p) {
+  f32x4 x;
+  if constexpr (FP8) {
+    const uint32_t bad = odd_bits<true>(*(GlobalU32)p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(bad >> (8 * i) & 1 ? 0x7fc00000u : 0u);
+  } else {
+    u32x2 w = *(GlobalU32x2)p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      w[i] &= odd_bits<false>(w[i]);
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  return x;
+}
+
+__device__ __forceinline__ int64_t lane_value(int64_t x, uint32_t lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// use(key, its values) for those keys of [lo, hi) whose values are not all
+// finite, by a wavefront.
+template <int D, bool FP8, class Use>
+__device__ __forceinline__ void odd_keys(const AttendArgs& a, const int32_t* table, GlobalBytes vp, uint32_t kv, int lo, int hi, Use use) {
+  constexpr uint32_t kRow = FP8 ? D : 2 * D;
+#pragma unroll 1
+  for (int k = lo; k < hi; k += 64) {
+    const uint32_t key = (uint32_t)min(k + (int)(threadIdx.x & 63), hi - 1), at = a.b.page.div(key), page = (uint32_t)table[at];
+    const bool fine = page < a.c.n_pages;
+    const int64_t off = (fine ? (int64_t)page * a.c.stride : 0) + (int64_t)(key - at * a.b.page.d) * (a.n_heads * kRow) + (int64_t)kv * kRow;
+    uint32_t bad = 0;
+#pragma unroll 1
+    for (uint32_t i = 0; i < kRow; i += 16) {
+      const u32x4 w = *(GlobalU32x4)(vp + off + i);
+      bad |= odd_bits<FP8>(w[0]) | odd_bits<FP8>(w[1]) | odd_bits<FP8>(w[2]) | odd_bits<FP8>(w[3]);
+    }
+    uint64_t some = __ballot(fine && bad && k + (int)(threadIdx.x & 63) < hi);
+#pragma unroll 1
+    for (; some; some &= some - 1) {
+      const uint32_t i = (uint32_t)__builtin_ctzll(some);
+      use(k + (int)i, vp + lane_value(off, i));
+    }
+  }
+}
+
 // ---- tiles of 16 rows -----------------------------------------------------------------
 // For few rows per request. Every key and value is used by 16 rows at most, so
 // the cache's bytes are what it costs: they go from memory to registers in the
@@ -361,11 +424,6 @@ __device__ __forceinline__ Ids16 ids16(const AttendArgs& a, const int32_t* table
   x.row = at - i * a.b.page.d;
   x.page = (uint32_t)table[i];
   return x;
-}
-
-__device__ __forceinline__ int64_t lane_value(int64_t x, uint32_t lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
-  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 template <int N>
@@ -433,7 +491,7 @@ struct Rows16 {
 
 template <int D, bool FP8, bool EVEN>
 __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, uint32_t kv, int key0, const Place& p, bool edge,
-                                        Rows16<D, FP8>& r) {
+                                        bool several, uint32_t& odd, Rows16<D, FP8>& r) {
   typedef Tile16<D, FP8> Tile;
   constexpr int N = 8 * Tile::kGroups;
   const uint32_t lane = threadIdx.x & 63, c = lane % 16, quad = lane / 16;
@@ -481,6 +539,15 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
         for (int j = 0; j < Tile::kVWords; ++j) t.v[i][j] = 0;
       }
     }
+    if (edge && several)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < Tile::kVWords; ++j) {
+          const uint32_t bad = odd_bits<FP8>(t.v[i][j]);
+          odd |= bad;
+          t.v[i][j] &= ~bad;
+        }
   }
   float top = x[0];
 #pragma unroll
@@ -567,9 +634,11 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   const int last_lo = a.window ? (int)max((int64_t)0, (int64_t)q.before + t1 - (int64_t)a.window) : 0;
 
   const int key0 = (int)(s.b0 + k0) * step + (int)sub * Tile::kKeys, last = (int)(s.b0 + k1 - 1) * step + (int)sub * Tile::kKeys;
+  const bool several = !a.all && t1 - t0 > 1;  // rows that see different keys
+  auto edge = [&](int key) { return key + Tile::kKeys > first_hi || key < last_lo; };
+  uint32_t odd = 0;
   if (s.hi > s.lo) {
     const int mine = (int)(lane & (Tile::kKeys - 1));
-    auto edge = [&](int key) { return key + Tile::kKeys > first_hi || key < last_lo; };
     Tile ta, tb;
     // Page ids are asked for two steps ahead and before the keys of the step
     // between: who waits for them does not wait for those.
@@ -587,13 +656,30 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     int key = key0;
     for (; key + step <= last; key += 2 * step) {  // no way out in between: it would have every load waited for
       next(key + step, tb);
-      block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), r);
+      block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), several, odd, r);
       next(key + 2 * step, ta);
-      block16<D, FP8, EVEN>(a, tb, kv, key + step, p, edge(key + step), r);
+      block16<D, FP8, EVEN>(a, tb, kv, key + step, p, edge(key + step), several, odd, r);
     }
-    if (key <= last) block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), r);
+    if (key <= last) block16<D, FP8, EVEN>(a, ta, kv, key, p, edge(key), several, odd, r);
   }
 
+  if (several && __any(odd)) {
+#pragma unroll 1
+    for (int key = key0; key <= last; key += step) {
+      if (!edge(key)) continue;
+      odd_keys<D, FP8>(a, table, vp, kv, max(key, s.lo), min(key + Tile::kKeys, s.hi), [&](int at, GlobalBytes v) {
+        if (at < p.lo || at >= p.hi) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int n = 0; n < E; n += 4) {
+            const f32x4 y = odd4<FP8>(v + ((quad * 4 + i) * E + n) * (FP8 ? 1 : 2));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.o[n + j][i] += y[j];
+          }
+      });
+    }
+  }
   float sum = r.s.sum;
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
@@ -709,7 +795,8 @@ struct LdsMany {
 
 typedef __attribute__((address_space(3))) const char* LdsAddress;
 typedef __attribute__((address_space(3))) u32x4* LdsU32x4;
-__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(LdsAddress)p; }
+// (the low half of a generic address is the one in shared memory)
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)p; }
 
 template <int R>
 struct Products;
@@ -866,13 +953,33 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
       }
     }
   };
+  // Blocks [plain_lo, plain_hi) hold keys that all rows of the tile see, and no
+  // page is missing: their values are kept as they are.
+  int plain_lo = 0, plain_hi = 0x7fffffff;
+  if (!a.all && kind.tile_rows > 1) {
+    plain_hi = max(0, q.before + (int)(cur.tile * kind.tile_rows) + 1 - block0) / KT;
+    const int t1 = (int)min(cur.tile * kind.tile_rows + kind.tile_rows, q.rows);
+    if (a.window) plain_lo = max(0, (int)max((int64_t)0, (int64_t)q.before + t1 - (int64_t)a.window) - block0 + KT - 1) / KT;
+  }
+  uint32_t odd = 0;
   auto keep_v = [&](uint32_t n) {
     if (!brings) return;
+    if ((int)n < plain_lo || (int)n >= plain_hi) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if (v_gone >> i & 1) vr[i] = u32x4{0, 0, 0, 0};  // whatever page 0 holds there, it may be NaN
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t bad = odd_bits<FP8>(vr[i][j]);
+          odd |= bad;
+          vr[i][j] &= ~bad;
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint32_t to = v_to + ((n & 1) * KT + i * kKeys) * D * 2;
-      u32x4 x = vr[i];
-      if (holes && (v_gone >> i & 1)) x = u32x4{0, 0, 0, 0};  // whatever page 0 holds there, it may be NaN
+      const u32x4 x = vr[i];
       if constexpr (FP8) {
         const float by = scale_value(scale_held(scale_of(v_word[i], kv)));
         u32x4 w[2];
@@ -1025,6 +1132,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
     fetch_k();
     find(1);
     holes = __syncthreads_or(gone);
+    if (holes) plain_hi = 0;
     if constexpr (WAVES == 8) {
       // Wavefronts 0 to 3 are a phase ahead. A step of theirs keeps K of the next
       // block and V of this one; the others', a phase later, those of the block
@@ -1083,6 +1191,24 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
       }
     }
   }
+
+  if (__syncthreads_or(odd))
+#pragma unroll 1
+    for (int n = 0; n < blocks; ++n) {
+      if (n >= plain_lo && n < plain_hi) continue;
+      const int key0 = block0 + n * KT;
+      odd_keys<D, FP8>(a, table, vp, kv, max(key0, s.lo), min(key0 + KT, s.hi), [&](int key, GlobalBytes v) {
+        if (key < row_lo || key >= row_hi) return;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int j = 0; j < S; j += 4) {
+            const f32x4 y = odd4<FP8>(v + (d * R + 2 * j + 4 * part) * (FP8 ? 1 : 2));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][j + i] += y[i];
+          }
+      });
+    }
 
   float sum = st.sum;
   if constexpr (R == 16) sum += __shfl_xor(sum, 16);

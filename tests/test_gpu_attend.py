@@ -156,6 +156,49 @@ def test_scales_at_their_ends():
     check(c, 2)
 
 
+ODD = [  # H, D, Hq, q_len, kv_len, window
+    (2, 64, 4, [5, 1], [60, 33], 0),
+    (2, 64, 8, [3, 2], [3, 200], 40),
+    (1, 64, 20, [2], [50], 0),
+    (2, 128, 8, [4], [4000], 0),
+    (2, 128, 8, [45, 3], [45, 100], 0),
+    (2, 128, 4, [300], [500], 0),
+    (2, 128, 4, [150, 2], [400, 90], 64),
+    (2, 128, 4, [150], [9000], 0),
+    (2, 256, 6, [3], [70], 0),
+    (1, 256, 6, [90], [130], 30),
+]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
+@pytest.mark.parametrize("H,D,Hq,q_len,kv_len,window", ODD)
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(cache, H, D, Hq, q_len, kv_len, window):
+    """NaN and infinite values, and NaN keys, among the new tokens and before them:
+    the rows that see them have them in the same elements, no other row has."""
+    c = Paged(26, 16, H, D, cache, q_len, kv_len, window).fill()
+    odd = [0x7FC0, 0x7F80, 0xFF80] if cache == "bf16" else [0x7F, 0xFF, 0x7F]
+    for i, (n, k) in enumerate(zip(q_len, kv_len)):
+        first = k - n
+        # a value before the new tokens only leaves the rows of a window
+        for m, at in enumerate([k - 1, k - 1, first + n // 2] + ([first - 3, first - window + n // 3] if window and first > window else [])):
+            c.codes(1)[c.table[i, at // 16], at % 16, m % H, 7 * m + 3] = odd[m % 3]
+        at = first + 2 * n // 3
+        if n > 1 and i == 0:
+            c.codes(0)[c.table[i, at // 16], at % 16, 0, 5] = odd[0]
+    c.up()
+    d, q = queries(c, Hq)
+    got, lse = run(c, d)
+    with np.errstate(invalid="ignore"):
+        want, wlse, tol, ltol = pc.attend(c, q, D ** -0.5)
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        fine = np.isfinite(want)
+        assert not fine.all() and fine.any()
+        assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+        assert (np.abs(got - want) <= tol)[fine].all()
+        assert np.array_equal(np.isnan(lse), np.isnan(wlse))
+        assert (np.abs(lse - wlse) <= ltol)[np.isfinite(wlse)].all()
+
+
 def test_strides_and_rows_of_no_request():
     c = Paged(18, 16, 2, 64, "bf16", [3, 50], [20, 90]).fill().up()
     Hq, n = 4, c.rows + 5
