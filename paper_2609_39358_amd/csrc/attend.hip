@@ -55,6 +55,7 @@ struct AttendArgs {
   float scale;               // times log2(e), above 0
   uint32_t q_sign;           // flips the signs of q for scales below 0
   uint32_t slot_rows;        // rows of a worker's part
+  uint32_t joins;            // workgroups that join a tile's parts
   Share* share;              // [workers]
   float* part_ml;            // [2 * workers][slot_rows][2]
   float* part_o;             // [2 * workers][slot_rows][D]
@@ -539,16 +540,16 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
         for (int j = 0; j < Tile::kVWords; ++j) t.v[i][j] = 0;
       }
     }
-    if (edge && several)
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int j = 0; j < Tile::kVWords; ++j) {
-          const uint32_t bad = odd_bits<FP8>(t.v[i][j]);
-          odd |= bad;
-          t.v[i][j] &= ~bad;
-        }
   }
+  if (edge && several)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::kVWords; ++j) {
+        const uint32_t bad = odd_bits<FP8>(t.v[i][j]);
+        odd |= bad;
+        t.v[i][j] &= ~bad;
+      }
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
@@ -1277,9 +1278,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
 
 // ---- joining ---------------------------------------------------------------------------
 // A tile that several workers share: the workgroups of the second of them add up
-// their parts. A run of D / 4 threads takes a row; where there are fewer rows than
-// runs, several take every so manieth of a row's parts. The order of the sums
-// follows from the sizes alone.
+// its parts, each those of some of its rows. A run of D / 4 threads takes a row;
+// where there are fewer rows than runs, several take every so manieth of a row's
+// parts. The order of the sums follows from the sizes alone.
 template <int D>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   constexpr uint32_t kLanes = D / 4, kRuns = 256 / kLanes;
@@ -1288,34 +1289,32 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     float top[kRuns], sum[kRuns];
     f32x4 y[kRuns][kLanes];
   } l;
-  const uint32_t split = a.slot_rows / kRuns;  // workgroups of a worker
-  const uint32_t worker = blockIdx.x / split + 1, row0 = blockIdx.x % split * kRuns;
+  const uint32_t worker = blockIdx.x / a.joins + 1;
   const Share sh = a.share[worker];
   if (!sh.parts) return;
   const Kind& kind = a.kind[sh.kind];
-  if (row0 >= kind.rows << kind.heads_shift) return;
   Request q = {};
   q.row0 = sh.row0;
   q.rows = sh.rows;
-  // rows [row0, row0 + kRuns) of the part: of one run of heads, m0 its first
-  const uint32_t head = (sh.head << kind.heads_shift) + row0 / kind.rows, m0 = row0 % kind.rows;
-  const uint32_t tokens = min(kind.tile_rows, sh.rows - sh.tile * kind.tile_rows), rows = tokens * kind.part_heads;
-  if (m0 >= rows) return;
+  // the tile's rows, one run of heads after another
+  const uint32_t rows = min(kind.tile_rows, sh.rows - sh.tile * kind.tile_rows) * kind.part_heads, all = rows << kind.heads_shift;
+  const uint32_t mine = (all + a.joins - 1) / a.joins, f0 = blockIdx.x % a.joins * mine, end = min(f0 + mine, all);
   uint32_t slices = kRuns;  // of a row's parts
-  while (slices > 1 && (rows - m0) * slices > kRuns) slices /= 2;
-  const uint32_t run = threadIdx.x / kLanes, d = threadIdx.x % kLanes, i = run / slices, slice = run % slices, m = m0 + i;
-  const Place p = place_of(a, kind, q, head, sh.tile, min(m, kind.rows - 1));
-  float top = kNone, sum = 0.f;
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  const bool there = p.there && m < kind.rows;
-  if (there) {
-    for (uint32_t w0 = slice; w0 < sh.parts; w0 += slices * kAhead) {
+  while (slices > 1 && mine * slices > kRuns) slices /= 2;
+  const uint32_t run = threadIdx.x / kLanes, d = threadIdx.x % kLanes, i = run / slices, slice = run % slices;
+  for (uint32_t f = f0; f < end; f += kRuns) {
+    const bool there = f + i < end;
+    const uint32_t at_head = min(f + i, end - 1) / rows, m = min(f + i, end - 1) % rows, row = at_head * kind.rows + m;
+    const Place p = place_of(a, kind, q, (sh.head << kind.heads_shift) + at_head, sh.tile, m);
+    float top = kNone, sum = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t w0 = slice; there && w0 < sh.parts; w0 += slices * kAhead) {
       f32x2 ml[kAhead];
       f32x4 o[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const uint32_t w = min(w0 + k * slices, sh.parts - 1);
-        const uint64_t at = (2 * (uint64_t)(worker - 1 + w) + (w == 0 ? 1 : 0)) * a.slot_rows + row0 + i;
+        const uint64_t at = (2 * (uint64_t)(worker - 1 + w) + (w == 0 ? 1 : 0)) * a.slot_rows + row;
         ml[k] = *(const f32x2*)(a.part_ml + at * 2);
         o[k] = *(const f32x4*)(a.part_o + at * D + 4 * d);
         if (w0 + k * slices >= sh.parts) ml[k][0] = kNone;
@@ -1330,37 +1329,37 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
         top = now;
       }
     }
-  }
-  if (slices > 1) {
-    if (d == 0) {
-      l.top[run] = top;
-      l.sum[run] = sum;
+    if (slices > 1) {  // then these are all of the workgroup's rows
+      if (d == 0) {
+        l.top[run] = top;
+        l.sum[run] = sum;
+      }
+      l.y[run][d] = y;
+      __syncthreads();
+      if (slice) return;
+      const float own = top;
+      for (uint32_t k = 1; k < slices; ++k) top = fmaxf(top, l.top[run + k]);
+      const float by0 = own == kNone ? 0.f : exp2_(own - top);
+      sum *= by0;
+      y *= by0;
+      for (uint32_t k = 1; k < slices; ++k) {
+        const float by = l.top[run + k] == kNone ? 0.f : exp2_(l.top[run + k] - top);
+        sum += l.sum[run + k] * by;
+        y += l.y[run + k][d] * by;
+      }
     }
-    l.y[run][d] = y;
-    __syncthreads();
-    if (slice) return;
-    const float mine = top;
-    for (uint32_t k = 1; k < slices; ++k) top = fmaxf(top, l.top[run + k]);
-    const float by0 = mine == kNone ? 0.f : exp2_(mine - top);
-    sum *= by0;
-    y *= by0;
-    for (uint32_t k = 1; k < slices; ++k) {
-      const float by = l.top[run + k] == kNone ? 0.f : exp2_(l.top[run + k] - top);
-      sum += l.sum[run + k] * by;
-      y += l.y[run + k][d] * by;
-    }
+    if (!there || !p.there) continue;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    store_bf16x4(a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head + 4 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+    if (a.lse && d == 0) a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(top, sum);
   }
-  if (!there) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  store_bf16x4(a.out + (int64_t)p.row * a.o_token + (int64_t)p.head * a.o_head + 4 * d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-  if (a.lse && d == 0) a.lse[(uint64_t)p.row * a.n_heads * a.group + p.head] = lse_of(top, sum);
 }
 
 // ---- launching ----------------------------------------------------------------------------
 struct Shape {
   uint32_t waves;      // of a workgroup; 0: k_attend16, else k_attend_many with so many
   uint32_t workers;    // workgroups: as many as the device holds at a time
-  uint32_t slot_rows;
+  uint32_t slot_rows, joins;
   Kind kind[2];
   uint32_t few;
 };
@@ -1401,6 +1400,21 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   m.cost = 4 * m.weight;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
+  // Tiles of many rows have few parts: a run of threads for each row. Tiles of few
+  // rows may have many, if there are few tiles: so many runs for a row that each
+  // has about 8 parts, which are on their way together. Four tiles of 8 rows of 128
+  // parts: 8.2 us, with 2 of a workgroup's 8 runs for each row 12.1.
+  const uint32_t runs_of_block = 1024 / ctx->D;
+  s.joins = s.slot_rows / runs_of_block;
+  if (!s.waves) {
+    const uint64_t reqs = n_reqs ? n_reqs : 1, tokens = (n_rows + reqs - 1) / reqs;
+    const uint64_t rows = (tokens < f.tile_rows ? tokens : f.tile_rows) * f.part_heads << f.heads_shift;
+    uint64_t slices = s.workers / (reqs * f.heads) / 8;
+    slices = slices < 1 ? 1 : slices > runs_of_block ? runs_of_block : slices;
+    const uint64_t wanted = (rows * slices + runs_of_block - 1) / runs_of_block;
+    if (wanted < s.joins) s.joins = (uint32_t)wanted;
+    if (!s.joins) s.joins = 1;
+  }
   return s;
 }
 
@@ -1429,7 +1443,7 @@ void launch(const Shape& sh, hipStream_t s, const AttendArgs& a) {
       hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 4>), grid, dim3(256), 0, s, a);
   }
   TimedLaunch timed(TL_KERNEL_ATTEND_JOIN, s);
-  hipLaunchKernelGGL((k_attend_join<D>), dim3((sh.workers - 1) * (a.slot_rows * D / 1024)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_attend_join<D>), dim3((sh.workers - 1) * sh.joins), dim3(256), 0, s, a);
 }
 
 template <int D>
@@ -1465,6 +1479,7 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
   a.kind[1] = sh.kind[1];
   a.few = sh.few;
   a.slot_rows = sh.slot_rows;
+  a.joins = sh.joins;
   a.all = (flags & TL_ATTEND_ALL) != 0;
   a.window = a.all ? 0 : (uint32_t)ctx->window[layer];
   const float by = scale * 1.4426950408889634f;
