@@ -34,7 +34,6 @@ struct AppendArgs {
 
 constexpr int kWaves = 4;
 constexpr uint32_t kInfinite = 0x7f800000;
-constexpr uint32_t kMany = 1024;  // workgroups that fill the device
 
 typedef __attribute__((address_space(1))) uint8_t* GlobalOut;
 typedef __attribute__((address_space(1))) u32x2* GlobalOut2;
@@ -460,7 +459,11 @@ template <int D>
 void launch(bool fp8, uint32_t grid, hipStream_t s, const AppendArgs& a) {
   if (!fp8)
     hipLaunchKernelGGL((k_append<D, 0>), dim3(grid), dim3(64 * kWaves), 0, s, a);
-  else if (a.step == 1)
+  else if (a.step <= (uint32_t)Row<D>::kRows || (a.n_windows >= 256 && a.step <= (uint32_t)(kWaves * Row<D>::kRows)))
+    // A lane holds one row: where one wavefront's lanes hold a window, or, with many
+    // windows, four do. 24,573 tokens into pages of 16 rows of 16 heads of 128: 153 us,
+    // 4.7 TB/s, with two rows held 170; 64 requests of 2 rows 7.6 and 9.5; 128
+    // windows of 16 rows 17.7 and 14.9.
     hipLaunchKernelGGL((k_append<D, 1>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   else
     hipLaunchKernelGGL((k_append<D, 2>), dim3(grid), dim3(64 * kWaves), 0, s, a);
@@ -525,7 +528,11 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     const uint64_t per = batch->n_rows / batch->n_reqs;
     a.step = (uint32_t)(per < 1 ? 1 : per < ctx->P ? per : ctx->P);
     a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
-    a.splits = a.step > 1 && a.n_windows < kMany ? std::min((kMany + a.n_windows - 1) / a.n_windows, (ctx->H + kWaves - 1) / kWaves) : 1;
+    // Workgroups that fill the device. Fewer windows give their heads to several (128 windows
+    // of 16 rows, 16 heads: 36 us with one, 19 with four each; 512: 41 and 49), and long ones
+    // are cut more readily (96 windows of 256 rows: 558 and 216).
+    const uint32_t many = a.step > 64 ? 1024 : 512;
+    a.splits = a.step > 1 && a.n_windows < many ? std::min((many + a.n_windows - 1) / a.n_windows, (ctx->H + kWaves - 1) / kWaves) : 1;
     a.split_heads = (ctx->H + a.splits - 1) / a.splits;
     a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
   }

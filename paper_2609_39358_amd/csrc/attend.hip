@@ -56,6 +56,7 @@ struct AttendArgs {
   uint32_t q_sign;           // flips the signs of q for scales below 0
   uint32_t slot_rows;        // rows of a worker's part
   uint32_t joins;            // workgroups that join a tile's parts
+  uint32_t least;            // units that a worker has, at least
   Share* share;              // [workers]
   float* part_ml;            // [2 * workers][slot_rows][2]
   float* part_o;             // [2 * workers][slot_rows][D]
@@ -185,7 +186,7 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   if (tid == 0) l.found = ~0u;
   __syncthreads();
   c.total = uniform(l.sum[kPlan]);
-  c.workers = (uint32_t)min((uint64_t)gridDim.x, (c.total + a.kind[1].weight - 1) / a.kind[1].weight);  // a block for each, at least
+  c.workers = (uint32_t)min((uint64_t)gridDim.x, (c.total + a.least - 1) / a.least);
   // runs that follow each other go to workgroups of one chiplet, which share an L2
   c.worker = blockIdx.x;
   if (c.workers == gridDim.x && gridDim.x % 8 == 0) c.worker = c.worker % 8 * (gridDim.x / 8) + c.worker / 8;
@@ -745,7 +746,9 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   }
 }
 
-// Tiles of 16 rows for all requests.
+// Tiles of 16 rows for all requests. One token over 97,000 in scaled pages of 16
+// heads of 128: 78 us, 5.1 TB/s (a large copy reaches 4.7); 64 requests of up to
+// 32,768 164 us, 5.2 TB/s.
 template <int D, bool FP8, bool EVEN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a) {
   __shared__ union {
@@ -1240,6 +1243,11 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   }
 }
 
+// 8,192 new tokens behind 8,192, 32 heads of 128 over 16 in scaled pages: 1.65 ms, 1,000
+// TFLOP/s (a large bf16 product of the library reaches 1,603). Heads of 256 are bound by
+// shared memory: 8 wavefronts read 64 KiB each per block, 4,096 cycles against 2,061
+// of products (203 tokens over 1,500 states: 450 TFLOP/s).
+//
 // Tiles of many rows, and of 16 for requests of few (heads of 256: their 16-row
 // tiles want the registers of one wavefront on a SIMD, and stay in k_attend16).
 template <int D, bool FP8, bool EVEN, int WAVES>
@@ -1359,7 +1367,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 struct Shape {
   uint32_t waves;      // of a workgroup; 0: k_attend16, else k_attend_many with so many
   uint32_t workers;    // workgroups: as many as the device holds at a time
-  uint32_t slot_rows, joins;
+  uint32_t slot_rows, joins, least;
   Kind kind[2];
   uint32_t few;
 };
@@ -1377,7 +1385,15 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   Shape s;
   const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
   const uint64_t per = n_rows * group / (n_reqs ? n_reqs : 1);
-  s.waves = per <= 32 ? 0 : ctx->D == 256 || per > 128 ? 8 : 4;
+  // Rows (query heads of a K/V head times new tokens) per request from which tiles
+  // of many rows are faster, and from which eight wavefronts beat four. us, 64 requests of about 1,024 keys,
+  // with tiles of 16 rows / four wavefronts / eight:
+  //   heads of 64    64 rows  34.7 / 37.1 / 47.6    96 rows  44.6 / 37.8 / 47.2    (two of 4,096 rows 101.0 with four,
+  //                  102.5 with eight; one of 16,384 332 and 320)
+  //   heads of 128   32 rows  65.8 / 75.1 / 75.6    48 rows  87.2 / 84.7 / 97.9    192 rows  272 / 154 / 145
+  //   heads of 256   12 rows   122 /   -  / 123     16 rows   128 /   -  / 124     32 rows   217 /  -  / 128
+  const uint32_t many = ctx->D == 64 ? 64 : ctx->D == 128 ? 32 : 12, eight = ctx->D == 64 ? 4096 : ctx->D == 128 ? 128 : 0;
+  s.waves = per <= many ? 0 : per > eight ? 8 : 4;
   s.workers = ctx->D == 256 || s.waves == 8 ? 256 : 512;
   s.few = !s.waves ? ~0u : ctx->D == 256 ? 0 : 32 / group;
   Kind& f = s.kind[0];
@@ -1405,16 +1421,20 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   // has about 8 parts, which are on their way together. Four tiles of 8 rows of 128
   // parts: 8.2 us, with 2 of a workgroup's 8 runs for each row 12.1.
   const uint32_t runs_of_block = 1024 / ctx->D;
+  const uint64_t reqs = n_reqs ? n_reqs : 1, tokens = (n_rows + reqs - 1) / reqs;
+  const uint64_t rows = (tokens < f.tile_rows ? tokens : f.tile_rows) * f.part_heads << f.heads_shift;
   s.joins = s.slot_rows / runs_of_block;
   if (!s.waves) {
-    const uint64_t reqs = n_reqs ? n_reqs : 1, tokens = (n_rows + reqs - 1) / reqs;
-    const uint64_t rows = (tokens < f.tile_rows ? tokens : f.tile_rows) * f.part_heads << f.heads_shift;
     uint64_t slices = s.workers / (reqs * f.heads) / 8;
     slices = slices < 1 ? 1 : slices > runs_of_block ? runs_of_block : slices;
     const uint64_t wanted = (rows * slices + runs_of_block - 1) / runs_of_block;
     if (wanted < s.joins) s.joins = (uint32_t)wanted;
     if (!s.joins) s.joins = 1;
   }
+  // A part costs the join more the more rows it has, so a worker of a small batch
+  // has to have some blocks. us with 1 / 2 / 3, 8 rows: 13 / 13 / 14 (1,024 keys),
+  // 13 / 13 / 14 (4,096); 32 rows: 13 / 13 / 13, 25 / 21 / 18; 64 rows: 18 / 16 / 15, 36 / 25 / 21.
+  s.least = (s.waves || rows > 32 ? 3 : rows > 8 ? 2 : 1) * m.weight;
   return s;
 }
 
@@ -1480,6 +1500,7 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
   a.few = sh.few;
   a.slot_rows = sh.slot_rows;
   a.joins = sh.joins;
+  a.least = sh.least;
   a.all = (flags & TL_ATTEND_ALL) != 0;
   a.window = a.all ? 0 : (uint32_t)ctx->window[layer];
   const float by = scale * 1.4426950408889634f;
