@@ -83,6 +83,22 @@ def test_append(cache, P, H, D, Hq, rot, axes, adjacent, q_len, kv_len, pad):
     same_pages(c, "again")
 
 
+SIDES = [  # P, H, D, q_len, held: both sides of the sizes where another kernel or launch is taken
+    (16, 2, 128, [16] * 258, 5),  # windows that four wavefronts hold one row a lane of
+    (16, 2, 128, [16] * 250, 5),  # fewer of them
+    (64, 1, 64, [64] * 258, 0),
+    (32, 4, 256, [16] * 258, 9),
+    (32, 4, 256, [32] * 258, 9),  # more rows than four wavefronts hold one a lane of
+    (16, 12, 64, [16] * 3, 30),  # heads on several workgroups
+    (256, 8, 128, [700], 100),
+]
+
+
+@pytest.mark.parametrize("P,H,D,q_len,held", SIDES)
+def test_append_on_both_sides_of_the_rules(P, H, D, q_len, held):
+    test_append("fp8_scaled", P, H, D, H, D, 1, False, q_len, [n + (held + i) % (2 * P) for i, n in enumerate(q_len)], 0)
+
+
 @pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
 def test_tokens_one_at_a_time_and_all_at_once_give_the_same_values(cache):
     # amplitudes that rise along the page: the scale rises with them

@@ -72,6 +72,29 @@ def test_attend(cache, P, H, D, Hq, q_len, kv_len, window, pad):
     check(c, Hq)
 
 
+SIDES = [  # P, H, D, Hq, q_len, kv_len: both sides of the sizes where other tiles or numbers of workgroups are taken
+    (16, 2, 64, 4, [32, 32], [300, 200]),
+    (16, 2, 64, 4, [33, 33], [300, 200]),
+    (16, 1, 64, 2, [2048], [2100]),
+    (16, 1, 64, 2, [2049], [2100]),
+    (16, 1, 128, 4, [8, 8], [1500, 60]),
+    (16, 1, 128, 4, [9, 9], [1500, 60]),
+    (16, 1, 128, 4, [33], [400]),
+    (32, 1, 256, 4, [3, 3], [900, 33]),
+    (32, 1, 256, 4, [4, 4], [900, 33]),
+    (16, 8, 64, 16, [1], [2000]),
+    (16, 8, 64, 64, [2], [2000]),
+    (16, 8, 128, 64, [2], [2000]),
+    (16, 8, 128, 64, [2] * 40, [100 + i for i in range(40)]),
+]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
+@pytest.mark.parametrize("P,H,D,Hq,q_len,kv_len", SIDES)
+def test_both_sides_of_the_rules(cache, P, H, D, Hq, q_len, kv_len):
+    check(Paged(28, P, H, D, cache, q_len, kv_len).fill(spread=1).up(), Hq)
+
+
 CROSS = [
     (16, 2, 64, 4, [1, 1, 5], [130, 0, 40], 0),
     (32, 3, 256, 6, [20, 33, 1], [75, 0, 31], 0),
