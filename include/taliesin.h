@@ -568,7 +568,8 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
  * that sees no key gets zeros. d_lse (device [n_rows][n_q_heads] floats, or
  * NULL) gets log(sum_j w_j), minus infinity for such a row.
  * Keys and values that are NaN or infinite reach the rows that see them, and no
- * others.
+ * others; a query that is NaN reaches its own row. A row whose scores are all
+ * minus infinity gets zeros, as if it saw no key.
  * Two kernels, no memset and no allocation. d_workspace: device, 16-byte
  * aligned, tl_attend_workspace_bytes(...) of it; needs no initialisation, and
  * calls that overlap need separate ones. out must not overlap q. */

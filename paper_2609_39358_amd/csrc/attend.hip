@@ -308,7 +308,9 @@ __device__ __forceinline__ void store_bf16x4(uint16_t* p, float x, float y, floa
 }
 
 // The running state of one row, on every lane that works for it. `top` is m, or
-// 0 while the row has seen nothing; `sum` a lane's own part.
+// 0 while the row has seen nothing; `sum` a lane's own part. Scores that are NaN
+// raise no maximum: a row (or a part of one) that has none has sums of 0, or NaN,
+// which count wherever parts are put together.
 struct Soft {
   float m, top, sum;
 };
@@ -736,7 +738,7 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     if (!pm.there) continue;
     float row_top = kNone, row_sum = 0.f, y[E];
     for (uint32_t w = h; w < WAVES; w += heads) row_top = fmaxf(row_top, l.m[w][m]);
-    for (uint32_t w = h; w < WAVES; w += heads) row_sum += l.m[w][m] == kNone ? 0.f : l.sum[w][m] * exp2_(l.m[w][m] - row_top);
+    for (uint32_t w = h; w < WAVES; w += heads) row_sum += l.m[w][m] == kNone ? l.sum[w][m] : l.sum[w][m] * exp2_(l.m[w][m] - row_top);
 #pragma unroll
     for (int n = 0; n < E; ++n) y[n] = 0.f;
     for (uint32_t w = h; w < WAVES; w += heads)
@@ -1325,11 +1327,15 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
         const uint64_t at = (2 * (uint64_t)(worker - 1 + w) + (w == 0 ? 1 : 0)) * a.slot_rows + row;
         ml[k] = *(const f32x2*)(a.part_ml + at * 2);
         o[k] = *(const f32x4*)(a.part_o + at * D + 4 * d);
-        if (w0 + k * slices >= sh.parts) ml[k][0] = kNone;
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        if (ml[k][0] == kNone) continue;
+        if (w0 + k * slices >= sh.parts) continue;
+        if (ml[k][0] == kNone) {  // zeros, or NaN
+          sum += ml[k][1];
+          y += o[k];
+          continue;
+        }
         const float now = fmaxf(top, ml[k][0]);
         const float old = top == kNone ? 0.f : exp2_(top - now), by = exp2_(ml[k][0] - now);
         sum = sum * old + ml[k][1] * by;
