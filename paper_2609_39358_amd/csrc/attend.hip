@@ -959,14 +959,17 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
       }
     }
   };
-  // Blocks [plain_lo, plain_hi) hold keys that all rows of the tile see, and no
-  // page is missing: their values are kept as they are.
-  int plain_lo = 0, plain_hi = 0x7fffffff;
-  if (!a.all && kind.tile_rows > 1) {
-    plain_hi = max(0, q.before + (int)(cur.tile * kind.tile_rows) + 1 - block0) / KT;
+  // Blocks [plain_lo, plain_hi) hold keys that all rows of the tile see, no copies of
+  // others (whose weight is 0, but 0 times infinity is NaN), and no page is missing:
+  // their values are kept as they are.
+  int all_from = s.lo, all_to = s.hi;
+  if (!a.all) {
     const int t1 = (int)min(cur.tile * kind.tile_rows + kind.tile_rows, q.rows);
-    if (a.window) plain_lo = max(0, (int)max((int64_t)0, (int64_t)q.before + t1 - (int64_t)a.window) - block0 + KT - 1) / KT;
+    all_to = min(all_to, q.before + (int)(cur.tile * kind.tile_rows) + 1);
+    if (a.window) all_from = max(all_from, (int)max((int64_t)0, (int64_t)q.before + t1 - (int64_t)a.window));
   }
+  const int plain_lo = max(0, all_from - block0 + KT - 1) / KT;
+  int plain_hi = max(0, all_to - block0) / KT;
   uint32_t odd = 0;
   auto keep_v = [&](uint32_t n) {
     if (!brings) return;
