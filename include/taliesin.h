@@ -492,7 +492,7 @@ int tl_chain_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_ch
  * replayed with other contents. Offsets are clamped to n_rows and lengths to
  * what a table row can address, so inconsistent arrays give fewer rows or keys,
  * never an access outside the arrays; offsets have to ascend. Rows that no
- * request owns are not written. */
+ * request owns are not written (one exception: q_out in tl_append). */
 typedef struct tl_batch {
   uint64_t n_reqs;            /* fewer than 2^20 */
   uint64_t n_rows;            /* rows of the row tensors, fewer than 2^24 */
@@ -551,7 +551,9 @@ typedef struct tl_rope {
  * row that no request owns, whose position is negative or has no place in the
  * table, or whose page id is outside [0, n_pages) (nothing is written to the
  * cache for these), or whose position has no angle (its key, value and query are
- * written as zeros). Rows of one call must not name one place twice, nor one
+ * written as zeros). The query of a row that no request owns is not written to
+ * q_out, unless rope->d_pos names a position for it that has an angle: then it is
+ * turned like any other. Rows of one call must not name one place twice, nor one
  * page from two requests. */
 int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
               const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,

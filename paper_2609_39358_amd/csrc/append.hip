@@ -387,6 +387,7 @@ __device__ void put_row(const AppendArgs& a, uint32_t t) {
     const bool fine = __all(has_place && g.ok);
     if (lane == 0) a.status[t] = fine ? TL_ACCEPT : TL_BADARG;
   }
+  if (r == a.b.n_reqs && !(a.pos && __all(g.ok))) return;  // not a request's row, and at no position of its own
   const GlobalOut k_row = (GlobalOut)*a.c.k + (int64_t)page * a.c.stride + (uint64_t)o * H * (2 * D);
   const GlobalOut v_row = (GlobalOut)*a.c.v + (int64_t)page * a.c.stride + (uint64_t)o * H * (2 * D);
   for (uint32_t u0 = lane / L; u0 < lines; u0 += kBatch * R) {
