@@ -573,8 +573,9 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
  * others; a query that is NaN reaches its own row. A row whose scores are all
  * minus infinity gets zeros, as if it saw no key.
  * Two kernels, no memset and no allocation. d_workspace: device, 16-byte
- * aligned, tl_attend_workspace_bytes(...) of it; needs no initialisation, and
- * calls that overlap need separate ones. out must not overlap q. */
+ * aligned, tl_attend_workspace_bytes(...) of it, which is enough for every call
+ * with so many query heads and at most so many requests and rows; needs no
+ * initialisation, and calls that overlap need separate ones. out must not overlap q. */
 #define TL_ATTEND_ALL 1
 size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t n_reqs, size_t n_rows);
 int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,

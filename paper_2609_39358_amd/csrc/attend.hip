@@ -11,6 +11,7 @@
 // The matrix instructions take bf16. A code times its power-of-two scale is a
 // bf16 value exactly; the weights 2^(s - m) are rounded to bf16 for the product
 // with v (as accurate as the bf16 output), and not for the sum.
+#include <algorithm>
 #include <type_traits>
 
 #include "paged.h"
@@ -1390,10 +1391,8 @@ Kind kind_of(const tl_ctx* ctx, uint32_t group, uint32_t rows) {
   return k;
 }
 
-Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
-  Shape s;
-  const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
-  const uint64_t per = n_rows * group / (n_reqs ? n_reqs : 1);
+// Wavefronts of a workgroup for requests of `per` rows on average.
+uint32_t waves_of(const tl_ctx* ctx, uint64_t per) {
   // Rows (query heads of a K/V head times new tokens) per request from which tiles
   // of many rows are faster, and from which eight wavefronts beat four. us, 64 requests of about 1,024 keys,
   // with tiles of 16 rows / four wavefronts / eight:
@@ -1402,7 +1401,13 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   //   heads of 128   32 rows  65.8 / 75.1 / 75.6    48 rows  87.2 / 84.7 / 97.9    192 rows  272 / 154 / 145
   //   heads of 256   12 rows   122 /   -  / 123     16 rows   128 /   -  / 124     32 rows   217 /  -  / 128
   const uint32_t many = ctx->D == 64 ? 64 : ctx->D == 128 ? 32 : 12, eight = ctx->D == 64 ? 4096 : ctx->D == 128 ? 128 : 0;
-  s.waves = per <= many ? 0 : per > eight ? 8 : 4;
+  return per <= many ? 0 : per > eight ? 8 : 4;
+}
+
+Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows, uint32_t waves) {
+  Shape s;
+  const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
+  s.waves = waves;
   s.workers = ctx->D == 256 || s.waves == 8 ? 256 : 512;
   s.few = !s.waves ? ~0u : ctx->D == 256 ? 0 : 32 / group;
   Kind& f = s.kind[0];
@@ -1447,6 +1452,10 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   return s;
 }
 
+Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
+  return shape_of(ctx, n_q_heads, n_reqs, n_rows, waves_of(ctx, n_rows * (n_q_heads / ctx->H) / (n_reqs ? n_reqs : 1)));
+}
+
 struct Layout {
   uint64_t ml, o, end;
 };
@@ -1455,7 +1464,7 @@ Layout layout_of(const Shape& s, uint32_t D) {
   const uint64_t rows = 2ull * s.workers * s.slot_rows;
   l.ml = ((uint64_t)s.workers * sizeof(Share) + 255) / 256 * 256;
   l.o = l.ml + rows * 2 * 4;
-  l.end = l.o + rows * D * 4;
+  l.end = (l.o + rows * D * 4 + 255) / 256 * 256;
   return l;
 }
 
@@ -1485,8 +1494,18 @@ void launch(bool fp8, bool even, const Shape& sh, hipStream_t s, const AttendArg
 
 }  // namespace
 
-size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
-  return (layout_of(shape_of(ctx, n_q_heads, n_reqs, n_rows), ctx->D).end + 255) / 256 * 256;
+size_t attend_needs(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
+  return layout_of(shape_of(ctx, n_q_heads, n_reqs, n_rows), ctx->D).end;
+}
+
+// The layout follows from the number of wavefronts alone, and fewer requests or
+// rows may take any that no more than all rows of one request ask for.
+size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_rows) {
+  const uint64_t most = std::min<uint64_t>(n_rows, 1u << 24) * (n_q_heads / ctx->H);
+  uint64_t need = 0;
+  for (uint32_t waves : {0u, 4u, 8u})
+    if (waves <= waves_of(ctx, most)) need = std::max(need, layout_of(shape_of(ctx, n_q_heads, 1, n_rows, waves), ctx->D).end);
+  return need;
 }
 
 int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads, const tl_rows* q,

@@ -114,7 +114,9 @@ int launch_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_chai
 int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
                   const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
                   const tl_cache* cache, uint8_t* d_status);
-size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows);
+// Bytes of workspace of one call, and of any call with at most so many rows.
+size_t attend_needs(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows);
+size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_rows);
 int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
                   const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
                   float* d_lse, void* d_ws);

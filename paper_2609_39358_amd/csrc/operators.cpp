@@ -85,9 +85,9 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
   return tl::launch_append(ctx, stream, layer, batch, rope, k, v, n_q_heads, q, q_out, cache, d_status);
 }
 
-size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t n_reqs, size_t n_rows) {
+size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t /*n_reqs*/, size_t n_rows) {
   if (!ctx || !heads_ok(ctx, n_q_heads)) return 0;
-  return tl::attend_workspace(ctx, n_q_heads, n_reqs, n_rows);
+  return tl::attend_workspace(ctx, n_q_heads, n_rows);
 }
 
 int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
@@ -101,7 +101,7 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
   if (batch->n_rows == 0 || batch->n_reqs == 0) return TL_OK;
   if (!rows_ok(q) || !result_ok(out, batch->n_rows, n_q_heads, ctx->D)) return TL_EINVAL;
   if (!d_workspace || ((uintptr_t)d_workspace & 15) || ((uintptr_t)d_lse & 3)) return TL_EINVAL;
-  if (workspace_bytes < tl_attend_workspace_bytes(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
+  if (workspace_bytes < tl::attend_needs(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
   return tl::launch_attend(ctx, stream, layer, batch, n_q_heads, q, cache, scale, flags, out, d_lse, d_workspace);
 }
 
