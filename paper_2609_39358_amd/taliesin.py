@@ -81,16 +81,20 @@ class tl_rope(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
-_BF16 = None  # torch's bf16, where torch is there
+# torch's types of the operators' arguments, where torch is there
+_BF16 = None
+_WORDS = _FLOATS = _BYTES = ()
 
 
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError("libtaliesin.so is not built (python -m paper_2609_39358_amd.build)")
-    global _BF16
+    global _BF16, _WORDS, _FLOATS, _BYTES
     try:  # bind the library's HIP calls to the runtime torch has already loaded
         import torch
         _BF16 = torch.bfloat16
+        _WORDS, _FLOATS = (torch.int32, torch.uint32, torch.uint8), (torch.float32,)
+        _BYTES = (torch.uint8, torch.int8, torch.bool)
     except ImportError:
         pass
     lib = ctypes.CDLL(LIB_PATH)
@@ -577,9 +581,19 @@ TL_ROPE_ADJACENT = 1
 TL_ATTEND_ALL = 1
 
 
+def _of_type(x, types: Sequence, what: str):
+    """A tensor argument of another element type would be read as something else.
+    (Bytes are taken as what the caller laid out in them.)"""
+    dtype = getattr(x, "dtype", None)
+    if dtype is not None and dtype not in types and hasattr(x, "data_ptr"):
+        raise ValueError("%s must be %s, got %s" % (what, str(types[0])[6:], dtype))  # torch.int32: int32
+
+
 def make_batch(n_reqs: int, n_rows: int, d_row_off, d_kv_len, d_tables, table_width: int) -> tl_batch:
     """One call's requests (tl_batch): d_row_off u32 [n_reqs + 1], d_kv_len
     u32 [n_reqs], d_tables i32 [n_groups, n_reqs, table_width], on the device."""
+    for x, what in ((d_row_off, "row offsets"), (d_kv_len, "cache lengths"), (d_tables, "page tables")):
+        _of_type(x, _WORDS, what)
     _fits(d_row_off, 4 * (n_reqs + 1), "row offsets")
     _fits(d_kv_len, 4 * n_reqs, "cache lengths")
     _fits(d_tables, 4 * n_reqs * table_width, "page tables")
@@ -595,6 +609,8 @@ def make_rope(d_cos_sin, rot_dim: int, d_pos=None, pair_axis: Optional[Sequence[
     their requests; pair_axis: the axis of each of the rot_dim / 2 pairs."""
     if pair_axis is not None and len(pair_axis) != rot_dim // 2:
         raise ValueError("%d axes for %d pairs" % (len(pair_axis), rot_dim // 2))
+    _of_type(d_cos_sin, _FLOATS, "angles")
+    _of_type(d_pos, _WORDS, "positions")
     n_angles = d_cos_sin.shape[0]
     _fits(d_cos_sin, 4 * n_angles * rot_dim, "angles")
     n_axes = 1 if d_pos is None or d_pos.dim() == 1 else d_pos.shape[0]
@@ -641,6 +657,7 @@ def tl_append(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, k,
         if q is None or q_out is None or q.shape != q_out.shape:
             raise ValueError("queries and rotated queries go together and have one shape")
         heads, q, q_out = q.shape[1], _rows(q, n, dim, "queries"), _rows(q_out, n, dim, "rotated queries")
+    _of_type(d_status, _BYTES, "status")
     _fits(d_status, n, "status")
     if rope is not None:
         keep = getattr(rope, "_keep", None)
@@ -664,6 +681,7 @@ def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q,
     n, dim, shape = batch.n_rows, ctx.head_dim, q.shape
     if shape != out.shape:
         raise ValueError("queries %s and results %s differ in shape" % (tuple(shape), tuple(out.shape)))
+    _of_type(lse, _FLOATS, "lse")
     _fits(lse, 4 * n * shape[1], "lse")
     _fits(d_workspace, workspace_bytes, "workspace")
     st = _lib.tl_attend(ctx.handle, _stream(stream), layer, batch, shape[1], _rows(q, n, dim, "queries"), cache,
