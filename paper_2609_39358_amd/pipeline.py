@@ -385,6 +385,7 @@ class NewTokens:
         self.cache, self._pages = cache.tl(), cache
         self.batch = T.make_batch(n, n_rows, d_row_off, d_kv_len, d_tables, width)
         self.rope = None if d_cos_sin is None else T.make_rope(d_cos_sin, 2 * d_cos_sin.shape[1])
+        self._outlive(d_row_off, d_kv_len, d_tables, d_cos_sin)
         dev = cache.k[0].device
         with _on(self.stream):
             self.ws_bytes = T.tl_attend_workspace_bytes(ctx, n_q_heads, n, n_rows)
@@ -392,14 +393,19 @@ class NewTokens:
             self.status = torch.empty(n_rows, dtype=torch.uint8, device=dev)
             self.q = torch.empty((n_rows, n_q_heads, ctx.head_dim), dtype=torch.bfloat16, device=dev)
 
+    def _outlive(self, *tensors):
+        """The caller may drop them (or this object) before the stream has read them."""
+        if self.stream != torch.cuda.current_stream():
+            for x in tensors:
+                if x is not None:
+                    x.record_stream(self.stream)
+
     def layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor = None) -> torch.Tensor:
         """q [n_rows, n_q_heads, D], k and v [n_rows, n_kv_heads, D] in bf16, as
         the model's projections left them (slices of one tensor will do). Returns
         [n_rows, n_q_heads, D]."""
         s = self.stream
-        if s != torch.cuda.current_stream():
-            for x in (q, k, v) + (() if lse is None else (lse,)):
-                x.record_stream(s)  # the caller may drop them before the stream has read them
+        self._outlive(q, k, v, lse)
         with _on(s):
             out = torch.empty_like(self.q)
             T.tl_append(self.ctx, s, l, self.batch, self.cache, k, v, self.rope, q, self.q, self.status)
