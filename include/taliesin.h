@@ -490,9 +490,9 @@ int tl_chain_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_ch
  * d_tables[group(layer)][r][p / page_tokens]. All three arrays are read on the
  * device when the kernels run: a call can be captured into a HIP graph, and
  * replayed with other contents. Offsets are clamped to n_rows and lengths to
- * what a table row can address, so inconsistent arrays give fewer rows or keys,
- * never an access outside the arrays; offsets have to ascend. Rows that no
- * request owns are not written (one exception: q_out in tl_append). */
+ * what a table row can address, 2^31 - 2^16 at most, so inconsistent arrays give
+ * fewer rows or keys, never an access outside the arrays; offsets have to ascend.
+ * Rows that no request owns are not written (one exception: q_out in tl_append). */
 typedef struct tl_batch {
   uint64_t n_reqs;            /* fewer than 2^20 */
   uint64_t n_rows;            /* rows of the row tensors, fewer than 2^24 */

@@ -480,7 +480,7 @@ void fill_batch(Batch& b, const tl_ctx* ctx, uint32_t layer, const tl_batch* bat
   b.width = (uint32_t)batch->table_width;
   b.table = batch->d_tables + (uint64_t)ctx->geo.group[layer] * batch->n_reqs * batch->table_width;
   const uint64_t most = batch->table_width * ctx->P;
-  b.most = most < 0x7fffffff ? (uint32_t)most : 0x7fffffff;
+  b.most = most < kMostTokens ? (uint32_t)most : kMostTokens;
   b.page.set(ctx->P);
 }
 

@@ -82,7 +82,7 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r) {
   const uint32_t row1 = a.b.first_row(r + 1), kv_len = a.b.kv_len[r];
   q.rows = row1 > q.row0 ? row1 - q.row0 : 0;
   q.held = a.c.n_pages ? (int)min(kv_len, a.b.most) : 0;
-  q.before = (int)min(kv_len, 0x7fffffffu) - (int)q.rows;
+  q.before = (int)min(kv_len, kMostTokens + (1u << 15)) - (int)q.rows;  // behind any table's end it does not matter how far
   q.kind = q.rows > a.few;
   q.tile_rows = q.kind ? a.kind[1].tile_rows : a.kind[0].tile_rows;
   q.heads = q.kind ? a.kind[1].heads : a.kind[0].heads;

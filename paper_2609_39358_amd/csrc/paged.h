@@ -37,13 +37,17 @@ struct FastDiv {
   __device__ __forceinline__ uint32_t div(uint32_t x) const { return mul ? __umulhi(x, mul) >> shift : x; }
 };
 
+// Tokens of a request, at most: keys are numbered in 32 bits with a sign, and a
+// kernel's steps look up to some blocks past the last one.
+constexpr uint32_t kMostTokens = (1u << 31) - (1u << 16);
+
 // One call's requests (tl_batch) for one layer.
 struct Batch {
   const uint32_t* row_off;
   const uint32_t* kv_len;
   const int32_t* table;  // of the layer's group
   uint32_t n_reqs, n_rows, width;
-  uint32_t most;         // tokens that a table row can address, below 2^31
+  uint32_t most;         // tokens that a table row can address, up to kMostTokens
   FastDiv page;
 
   __device__ __forceinline__ uint32_t first_row(uint32_t r) const { return min(row_off[r], n_rows); }
