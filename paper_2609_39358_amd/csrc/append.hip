@@ -528,6 +528,9 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     // with few of those, some of the heads.
     const uint64_t per = batch->n_rows / batch->n_reqs;
     a.step = (uint32_t)(per < 1 ? 1 : per < ctx->P ? per : ctx->P);
+    // A launch has fewer than 2^32 threads: of millions of rows on pages of one token, a
+    // window takes four, one after another.
+    if (a.step == 1 && a.b.n_rows > (1u << 22)) a.step = 4;
     a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
     // Workgroups that fill the device. Fewer windows give their heads to several (128 windows
     // of 16 rows, 16 heads: 36 us with one, 19 with four each; 512: 41 and 49), and long ones
