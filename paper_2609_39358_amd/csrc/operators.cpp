@@ -41,7 +41,8 @@ bool rows_ok(const tl_rows* r) {
 // Results: no two of them in one place.
 bool result_ok(const tl_rows* r, uint64_t n_rows, uint32_t n_heads, uint32_t dim) {
   if (!rows_ok(r)) return false;
-  const int64_t row = r->row_stride, head = r->head_stride, d = dim, rows = (int64_t)n_rows, heads = n_heads;
+  // strides of up to 2^40 times rows of up to 2^24 pass 64 bits
+  const __int128 row = r->row_stride, head = r->head_stride, d = dim, rows = n_rows, heads = n_heads;
   if (row < 0 || head < 0) return false;
   const bool rows_outside = (heads == 1 || head >= d) && (rows == 1 || row >= (heads - 1) * head + d);
   const bool heads_outside = (rows == 1 || row >= d) && (heads == 1 || head >= (rows - 1) * row + d);
