@@ -546,6 +546,8 @@ typedef struct tl_rope {
  * the first one that is written are rounded again. Values that are not finite
  * become NaN codes. Powers of two make the scaling exact: a value is rounded to
  * e4m3 once, and a second time only below the smallest normal code after a rise.
+ * Finite values of 248 * 2^120 and more in magnitude (bf16's eight largest) round
+ * to 256 * 2^120, which bf16 and f32 hold as infinite.
  *
  * d_status (device [n_rows] or NULL): TL_ACCEPT for each row, or TL_BADARG for a
  * row that no request owns, whose position is negative or has no place in the

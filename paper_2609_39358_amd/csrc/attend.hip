@@ -1249,10 +1249,14 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   }
 }
 
-// 8,192 new tokens behind 8,192, 32 heads of 128 over 16 in scaled pages: 1.65 ms, 1,000
-// TFLOP/s (a large bf16 product of the library reaches 1,603). Heads of 256 are bound by
-// shared memory: 8 wavefronts read 64 KiB each per block, 4,096 cycles against 2,061
-// of products (203 tokens over 1,500 states: 450 TFLOP/s).
+// 8,192 new tokens behind 8,192, 32 heads of 128 over 16 in scaled pages: 1.71 ms, 966
+// TFLOP/s (a large bf16 product of the library reaches 1,603). The matrix units are
+// busy for 46 % of its cycles, the vector units for 52 %, shared memory for 37 %: the
+// phases of a SIMD's two wavefronts overlap little. Heads of 256 (203 tokens over
+// 1,500 states: 427 TFLOP/s) have them busy for 18, 28 and 26 %: a workgroup has about
+// one tile, and its start, its end and the barriers of some 20 blocks are what it waits for.
+// Registers that the compiler spills (heads of 128: 48 to 78 a lane) are used where a
+// tile starts and ends, not in the loop over blocks.
 //
 // Tiles of many rows, and of 16 for requests of few (heads of 256: their 16-row
 // tiles want the registers of one wavefront on a SIMD, and stay in k_attend16).
@@ -1409,6 +1413,11 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
   s.waves = waves;
   s.workers = ctx->D == 256 || s.waves == 8 ? 256 : 512;
+  // In the kernel that holds both kinds, requests with up to 32 rows take tiles of 16.
+  // us, two prompts of 330 tokens beside 60 requests of 4 / 8 / 16 tokens, 4 query heads a
+  // K/V head, 4,096 keys each: all in tiles of many rows 249 / 251 / 253, up to 16 rows
+  // in tiles of 16 179 / 251 / 253, up to 32 179 / 272 / 253, up to 64 179 / 272 / 422; beside 6 of
+  // 4 tokens 109, 88, 88, 88.
   s.few = !s.waves ? ~0u : ctx->D == 256 ? 0 : 32 / group;
   Kind& f = s.kind[0];
   f = kind_of(ctx, group, 16);
@@ -1418,7 +1427,8 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   f.heads = runs >> f.heads_shift;
   // keys of a wavefront's step, and how many wavefronts take steps of one run
   f.block_shift = (ctx->D * wide < 128 ? 6 : 5) + (s.waves == 8 ? 3 : 2) - f.heads_shift;
-  // A block of many rows takes about 1.5 times as long as one of few.
+  // A block of many rows counts for 1.5 of few. us with 1 / 1.5 / 2: two prompts of 330 beside
+  // 6 requests of 1 token 91 / 89 / 106, beside 60 169 / 173 / 186 (heads of 64, 8 of each: 164 / 194 / 231).
   f.weight = s.waves ? 2 : 1;
   f.cost = f.weight;
   Kind& m = s.kind[1];
@@ -1427,6 +1437,8 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   m.heads = ctx->H * m.parts;
   m.block_shift = 6;
   m.weight = s.waves ? 3 : 1;
+  // Finding a tile, its queries and its result count for 4 blocks. us with 1 / 4 / 8: 8 prompts of
+  // 200 tokens behind 100 51 / 35 / 35, 30 of 300 behind 500 198 / 192 / 187, the two of 330 91 / 89 / 91.
   m.cost = 4 * m.weight;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
