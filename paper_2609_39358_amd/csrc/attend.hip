@@ -1249,11 +1249,11 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   }
 }
 
-// 8,192 new tokens behind 8,192, 32 heads of 128 over 16 in scaled pages: 1.71 ms, 966
+// 8,192 new tokens behind 8,192, 32 heads of 128 over 16 in scaled pages: 1.7 ms, 960
 // TFLOP/s (a large bf16 product of the library reaches 1,603). The matrix units are
 // busy for 46 % of its cycles, the vector units for 52 %, shared memory for 37 %: the
 // phases of a SIMD's two wavefronts overlap little. Heads of 256 (203 tokens over
-// 1,500 states: 427 TFLOP/s) have them busy for 18, 28 and 26 %: a workgroup has about
+// 1,500 states: 430 TFLOP/s) have them busy for 18, 28 and 26 %: a workgroup has about
 // one tile, and its start, its end and the barriers of some 20 blocks are what it waits for.
 // Registers that the compiler spills (heads of 128: 48 to 78 a lane) are used where a
 // tile starts and ends, not in the loop over blocks.
