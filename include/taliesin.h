@@ -584,6 +584,81 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
               const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
               float* d_lse, void* d_workspace, size_t workspace_bytes);
 
+/* ---- pages of a cache ---------------------------------------------------------
+ * Requests that branch (several answers to one prompt, beams) share the pages that
+ * they have in common. These calls work on whole pages of every layer at once, of
+ * contexts of any type; each layer uses the tables of its group.
+ *
+ * A pool counts how many table rows name each page; a page that none names is free.
+ * Counts start as the caller sets them (0 for free pages; a page that must never be
+ * given out: 1). Counts of 0 and less are free. Which pages a call gives depends on
+ * the counts and the requests' order alone: the lowest free ones. */
+typedef struct tl_pool {
+  int32_t* d_refs; /* device [n_groups][n_pages] */
+  int64_t n_pages; /* as in tl_cache */
+} tl_pool;
+
+/* Copies page d_src[group][i] to d_dst[group][i] in every layer of that group (device
+ * [n_groups][n]; ids outside [0, n_pages), such as -1: not in that group): its first
+ * d_rows[i] tokens (device [n] or NULL: all of them) and, on scaled pages, its scales.
+ * Other rows of the page stay as they are. A call's sources and destinations must be
+ * different pages. One kernel, no workspace. */
+int tl_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, size_t n, const int32_t* d_src,
+                  const int32_t* d_dst, const uint32_t* d_rows);
+
+/* n new branches: branch i continues request d_parent[i] of n_parents, which holds
+ * d_kv_len[parent] tokens on the pages of its table row (device
+ * [n_groups][n_parents][table_width]). It shares the parent's full pages (each counts one
+ * more owner), and gets a page of its own for the last one if that is partly filled,
+ * with a copy of its rows. Its row of d_tables_out (device [n_groups][n][table_width],
+ * not overlapping d_tables) names these and -1 behind them; d_len_out[i] is its length.
+ * Entries of the parent's that name no page stay -1. d_status (device [n] or NULL):
+ * TL_ACCEPT; TL_BADARG for a parent outside [0, n_parents) or longer than its row;
+ * TL_MISSING where the pool has no page left for it, as branches are served in order
+ * (both: a row of -1, length 0, nothing is counted). Two kernels. */
+int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl_cache* cache, size_t n_parents,
+                  const uint32_t* d_kv_len, const int32_t* d_tables, size_t n, const int32_t* d_parent,
+                  uint32_t* d_len_out, int32_t* d_tables_out, size_t table_width, uint8_t* d_status,
+                  void* d_workspace, size_t workspace_bytes);
+
+/* Pages for more tokens: each of the entries of request i's table row between
+ * d_have[i] and d_want[i] tokens (the pages that begin there) that names no page gets a
+ * free one, in every group. d_status (device [n] or NULL): TL_ACCEPT; TL_BADARG where
+ * d_want is past the table row; TL_MISSING where what is left does not suffice, as
+ * requests are served in order (both: nothing is taken for it). One kernel. */
+int tl_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, const uint32_t* d_have,
+                  const uint32_t* d_want, int32_t* d_tables, size_t table_width, uint8_t* d_status,
+                  void* d_workspace, size_t workspace_bytes);
+
+/* Gives back what the n table rows name: all of it, or the pages that lie wholly within
+ * tokens [d_first[i], d_end[i]) (device [n] or NULL: from 0; to the row's end). Each
+ * entry counts one owner less and becomes -1. For rows that are dropped: both NULL; for a
+ * request cut down to a length: that as d_first; for what a sliding window has left
+ * behind: the window's start as d_end. One kernel, no workspace. */
+int tl_pages_free(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, int32_t* d_tables,
+                  size_t table_width, const uint32_t* d_first, const uint32_t* d_end);
+
+/* Workspace (device, 16-byte aligned) of tl_pages_fork and tl_pages_take for at most n
+ * branches or requests; calls that overlap need separate ones. */
+size_t tl_pages_workspace_bytes(const tl_ctx* ctx, size_t n, size_t n_pages);
+
+/* Rows that stay: of request r's new tokens (the batch as it was appended), those that
+ * d_keep[d_row_off[r] + i], i < d_n_keep[r], name by their number among them, ascending,
+ * move together, in every layer: new token d_keep[..][i] becomes new token i (drafted
+ * tokens that were accepted; the first and last tokens of a long request). On scaled
+ * pages a row's values are written as tl_append writes them (from the first row on that
+ * moves): a code is moved as it is where the scales agree, and rounded again where they
+ * do not. What lies behind the last kept token is not defined. Pages that a kept token
+ * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs], not
+ * overlapping d_kv_len) becomes the request's length. d_status (device [n_reqs] or NULL):
+ * TL_ACCEPT, or TL_BADARG where an entry is not larger than the one before, names no new
+ * token, or needs a page that the tables do not name: the tokens before that entry are
+ * kept, in all layers, and d_len_out says how many; or where d_kv_len is less than the
+ * request's rows or more than its table row holds: nothing moves, and d_len_out is
+ * d_kv_len. One kernel, no workspace. */
+int tl_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32_t* d_n_keep, const uint32_t* d_keep,
+            const tl_cache* cache, uint32_t* d_len_out, uint8_t* d_status);
+
 /* ---- record files: the disk tier ------------------------------------------
  * Records of one context kept back to back in one file (record id i at byte
  * offset i * record_bytes). Batches of whole records move between the file
@@ -630,7 +705,10 @@ int tl_file_drop_cache(tl_file* f);
 #define TL_KERNEL_APPEND 8
 #define TL_KERNEL_ATTEND 9
 #define TL_KERNEL_ATTEND_JOIN 10
-#define TL_KERNEL_COUNT 11
+#define TL_KERNEL_PAGES 11 /* tl_pages_copy, and the copies of tl_pages_fork */
+#define TL_KERNEL_POOL 12  /* what is taken from and given back to a pool */
+#define TL_KERNEL_KEEP 13
+#define TL_KERNEL_COUNT 14
 int tl_timing(int enable);
 int tl_timing_read(int kernel, double* total_ms, uint64_t* count);
 

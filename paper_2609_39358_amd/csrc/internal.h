@@ -121,6 +121,20 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
                   const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
                   float* d_lse, void* d_ws);
 
+// Pages as a whole; pages.hip.
+uint64_t pages_workspace(const tl_ctx* ctx, uint64_t n, uint64_t n_pages);
+int launch_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, uint64_t n, const int32_t* d_src,
+                      const int32_t* d_dst, const uint32_t* d_rows);
+int launch_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl_cache* cache, uint64_t n_parents,
+                      const uint32_t* d_kv_len, const int32_t* d_tables, uint64_t n, const int32_t* d_parent, uint32_t* d_len_out,
+                      int32_t* d_tables_out, uint64_t width, uint8_t* d_status, void* d_ws);
+int launch_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, uint64_t n, const uint32_t* d_have, const uint32_t* d_want,
+                      int32_t* d_tables, uint64_t width, uint8_t* d_status, void* d_ws);
+int launch_pages_free(const tl_ctx* ctx, void* stream, const tl_pool* pool, uint64_t n, int32_t* d_tables, uint64_t width,
+                      const uint32_t* d_first, const uint32_t* d_end);
+int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32_t* d_n_keep, const uint32_t* d_keep,
+                const tl_cache* cache, uint32_t* d_len_out, uint8_t* d_status);
+
 // Brackets one kernel launch with a pair of HIP events on `stream` while
 // timing is enabled (tl_timing); kernels.hip.
 class TimedLaunch {

@@ -1,5 +1,5 @@
-// Argument validation of the operators on a paged cache (tl_append, tl_attend),
-// in front of their launches.
+// Argument validation of the operators on a paged cache (tl_append, tl_attend,
+// tl_pages_*, tl_keep), in front of their launches.
 #include <math.h>
 
 #include "internal.h"
@@ -8,15 +8,47 @@ namespace {
 
 constexpr uint32_t kMaxHeads = 1u << 16;  // query heads
 
-// Caches that the operators read and write: bf16 pages, or scaled 8-bit ones.
-int check_layer(const tl_ctx* ctx, uint32_t layer, const tl_cache* c) {
-  if (layer >= ctx->L) return TL_EINVAL;
-  if (ctx->dtype != TL_DTYPE_BF16 && ctx->dtype != TL_DTYPE_FP8_SCALED) return TL_ELAYOUT;
-  if (ctx->D != 64 && ctx->D != 128 && ctx->D != 256) return TL_ELAYOUT;
+int check_cache(const tl_ctx* ctx, const tl_cache* c) {
   if (!c || !c->d_layer_k || !c->d_layer_v) return TL_EINVAL;
   if (c->page_stride < (int64_t)ctx->geo.slab_bytes || c->page_stride % 16) return TL_EINVAL;
   if (c->n_pages < 0 || c->n_pages > 0x7fffffff) return TL_EINVAL;
   if (((uintptr_t)c->d_layer_k | (uintptr_t)c->d_layer_v) & 7) return TL_EINVAL;
+  return TL_OK;
+}
+
+// Caches whose values the operators read and write: bf16 pages, or scaled 8-bit ones.
+int check_values(const tl_ctx* ctx) {
+  if (ctx->dtype != TL_DTYPE_BF16 && ctx->dtype != TL_DTYPE_FP8_SCALED) return TL_ELAYOUT;
+  if (ctx->D != 64 && ctx->D != 128 && ctx->D != 256) return TL_ELAYOUT;
+  return TL_OK;
+}
+
+int check_layer(const tl_ctx* ctx, uint32_t layer, const tl_cache* c) {
+  if (layer >= ctx->L) return TL_EINVAL;
+  const int r = check_values(ctx);
+  return r ? r : check_cache(ctx, c);
+}
+
+// A page's bytes are counted in 32 bits.
+int check_pages(const tl_ctx* ctx, const tl_cache* c) {
+  if (ctx->geo.slab_bytes >= (1ull << 31)) return TL_ELAYOUT;
+  return check_cache(ctx, c);
+}
+
+bool words_ok(const void* p) { return p && !((uintptr_t)p & 3); }
+bool maybe_words(const void* p) { return !((uintptr_t)p & 3); }
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
+int check_pool(const tl_pool* p) {
+  if (!p || !words_ok(p->d_refs) || p->n_pages < 0 || p->n_pages > 0x7fffffff) return TL_EINVAL;
+  return TL_OK;
+}
+
+// Table rows of a call: their entries are counted in 32 bits.
+int check_table_rows(uint64_t n, uint64_t width) {
+  if (n >= (1ull << 20) || width >= (1ull << 28) || n * width >= (1ull << 31)) return TL_ERANGE;
   return TL_OK;
 }
 
@@ -104,6 +136,81 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
   if (!d_workspace || ((uintptr_t)d_workspace & 15) || ((uintptr_t)d_lse & 3)) return TL_EINVAL;
   if (workspace_bytes < tl::attend_needs(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
   return tl::launch_attend(ctx, stream, layer, batch, n_q_heads, q, cache, scale, flags, out, d_lse, d_workspace);
+}
+
+int tl_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, size_t n, const int32_t* d_src,
+                  const int32_t* d_dst, const uint32_t* d_rows) {
+  if (!ctx) return TL_EINVAL;
+  const int r = check_pages(ctx, cache);
+  if (r) return r;
+  if (n >= (1ull << 24)) return TL_ERANGE;
+  if (!n) return TL_OK;
+  if (!words_ok(d_src) || !words_ok(d_dst) || !maybe_words(d_rows)) return TL_EINVAL;
+  return tl::launch_pages_copy(ctx, stream, cache, n, d_src, d_dst, d_rows);
+}
+
+size_t tl_pages_workspace_bytes(const tl_ctx* ctx, size_t n, size_t n_pages) {
+  if (!ctx || n >= (1ull << 20) || n_pages > 0x7fffffff) return 0;
+  return tl::pages_workspace(ctx, n, n_pages);
+}
+
+int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl_cache* cache, size_t n_parents,
+                  const uint32_t* d_kv_len, const int32_t* d_tables, size_t n, const int32_t* d_parent,
+                  uint32_t* d_len_out, int32_t* d_tables_out, size_t table_width, uint8_t* d_status,
+                  void* d_workspace, size_t workspace_bytes) {
+  if (!ctx) return TL_EINVAL;
+  int r = check_pages(ctx, cache);
+  if (r || (r = check_pool(pool))) return r;
+  if (pool->n_pages != cache->n_pages) return TL_EINVAL;
+  if ((r = check_table_rows(n, table_width)) || (r = check_table_rows(n_parents, table_width))) return r;
+  if (!n) return TL_OK;
+  if (!words_ok(d_parent) || !words_ok(d_len_out) || (n_parents && !words_ok(d_kv_len))) return TL_EINVAL;
+  const uint64_t row = 4ull * ctx->geo.n_groups * table_width;
+  if (table_width && (!words_ok(d_tables_out) || (n_parents && !words_ok(d_tables)))) return TL_EINVAL;
+  if (overlap(d_tables_out, n * row, d_tables, n_parents * row) || overlap(d_len_out, 4 * n, d_kv_len, 4 * n_parents) ||
+      overlap(d_len_out, 4 * n, d_parent, 4 * n))
+    return TL_EINVAL;
+  if (!d_workspace || ((uintptr_t)d_workspace & 15)) return TL_EINVAL;
+  if (workspace_bytes < tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages)) return TL_ERANGE;
+  return tl::launch_pages_fork(ctx, stream, pool, cache, n_parents, d_kv_len, d_tables, n, d_parent, d_len_out,
+                               d_tables_out, table_width, d_status, d_workspace);
+}
+
+int tl_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, const uint32_t* d_have,
+                  const uint32_t* d_want, int32_t* d_tables, size_t table_width, uint8_t* d_status,
+                  void* d_workspace, size_t workspace_bytes) {
+  if (!ctx) return TL_EINVAL;
+  int r = check_pool(pool);
+  if (r || (r = check_table_rows(n, table_width))) return r;
+  if (!n) return TL_OK;
+  if (!words_ok(d_have) || !words_ok(d_want) || (table_width && !words_ok(d_tables))) return TL_EINVAL;
+  if (!d_workspace || ((uintptr_t)d_workspace & 15)) return TL_EINVAL;
+  if (workspace_bytes < tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages)) return TL_ERANGE;
+  return tl::launch_pages_take(ctx, stream, pool, n, d_have, d_want, d_tables, table_width, d_status, d_workspace);
+}
+
+int tl_pages_free(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, int32_t* d_tables,
+                  size_t table_width, const uint32_t* d_first, const uint32_t* d_end) {
+  if (!ctx) return TL_EINVAL;
+  int r = check_pool(pool);
+  if (r || (r = check_table_rows(n, table_width))) return r;
+  if (!n || !table_width) return TL_OK;
+  if (!words_ok(d_tables) || !maybe_words(d_first) || !maybe_words(d_end)) return TL_EINVAL;
+  return tl::launch_pages_free(ctx, stream, pool, n, d_tables, table_width, d_first, d_end);
+}
+
+int tl_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32_t* d_n_keep, const uint32_t* d_keep,
+            const tl_cache* cache, uint32_t* d_len_out, uint8_t* d_status) {
+  if (!ctx) return TL_EINVAL;
+  int r = check_values(ctx);
+  if (r || (r = check_pages(ctx, cache)) || (r = check_batch(batch))) return r;
+  if (!batch->n_reqs) return TL_OK;
+  if (!words_ok(batch->d_row_off) || !words_ok(batch->d_kv_len)) return TL_EINVAL;
+  if (!words_ok(d_n_keep) || !words_ok(d_len_out) || (batch->n_rows && !words_ok(d_keep))) return TL_EINVAL;
+  if (overlap(d_len_out, 4 * batch->n_reqs, batch->d_kv_len, 4 * batch->n_reqs) ||
+      overlap(d_len_out, 4 * batch->n_reqs, d_n_keep, 4 * batch->n_reqs))
+    return TL_EINVAL;
+  return tl::launch_keep(ctx, stream, batch, d_n_keep, d_keep, cache, d_len_out, d_status);
 }
 
 }  // extern "C"

@@ -1,0 +1,748 @@
+// Pages of a cache as a whole: copied (tl_pages_copy), shared and copied by new
+// branches of a request (tl_pages_fork), taken from and given back to a pool
+// (tl_pages_take, tl_pages_free), and the rows of a request that stay moved
+// together in them (tl_keep). All layers in one call.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace tl {
+namespace {
+
+// All layers' pages. A slab is one layer's K (2 * layer) or V (2 * layer + 1).
+struct Slabs {
+  const uint64_t* k;
+  const uint64_t* v;
+  int64_t stride;
+  uint32_t n_pages, n_slabs;
+  uint32_t page_tokens, row_bytes;
+  uint32_t code_bytes, n_scales;  // of a page; scale bytes follow its codes
+  uint32_t n_groups;
+  uint8_t group[TL_MAX_LAYERS];
+
+  __device__ __forceinline__ uint8_t* base(uint32_t slab) const { return (uint8_t*)(slab & 1 ? v : k)[slab >> 1]; }
+};
+
+typedef __attribute__((address_space(1))) uint8_t* Bytes;
+typedef __attribute__((address_space(1))) u32x4* Granules;
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kFlight = 4;                               // 16-byte pieces of a thread on their way
+constexpr uint32_t kPiece = kThreads * kFlight * 16;          // bytes that a workgroup copies at a time
+constexpr uint32_t kMostGroups = 1u << 22;                    // workgroups of a launch; further work is looped over
+
+// ---- copying ---------------------------------------------------------------------
+// One workgroup's piece of a page's first `rows` rows, and of its scales with the
+// first piece. Bounded by memory: every byte is read and written once.
+__device__ __forceinline__ void copy_piece(const Slabs& c, uint32_t slab, uint32_t src, uint32_t dst, uint32_t rows, uint32_t piece) {
+  const Bytes base = (Bytes)c.base(slab);
+  const Bytes from = base + (int64_t)src * c.stride, to = base + (int64_t)dst * c.stride;
+  const uint32_t bytes = rows * c.row_bytes, whole = bytes & ~15u, tid = threadIdx.x;
+  const uint32_t at = piece * kPiece + tid * 16;
+  u32x4 x[kFlight];
+#pragma unroll
+  for (uint32_t i = 0; i < kFlight; ++i)
+    if (at + i * kThreads * 16 < whole) x[i] = *(Granules)(from + at + i * kThreads * 16);
+#pragma unroll
+  for (uint32_t i = 0; i < kFlight; ++i)
+    if (at + i * kThreads * 16 < whole) *(Granules)(to + at + i * kThreads * 16) = x[i];
+  if (piece) return;
+  if (whole + tid < bytes) to[whole + tid] = from[whole + tid];  // rows that end within sixteen bytes
+  for (uint32_t i = tid; i < c.n_scales; i += kThreads) to[c.code_bytes + i] = from[c.code_bytes + i];
+}
+
+__host__ __device__ __forceinline__ uint32_t pieces_of(uint32_t bytes) { return bytes < kPiece ? 1 : (bytes + kPiece - 1) / kPiece; }
+
+struct CopyArgs {
+  Slabs c;
+  const int32_t* src;
+  const int32_t* dst;  // [n_groups][n]
+  const uint32_t* rows;
+  uint32_t n, pieces;
+};
+
+__global__ __launch_bounds__(kThreads) void k_pages_copy(CopyArgs a) {
+  const uint64_t per = (uint64_t)a.c.n_slabs * a.pieces, items = a.n * per;
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t i = (uint32_t)(item / per), rest = (uint32_t)(item % per), slab = rest / a.pieces, piece = rest % a.pieces;
+    const uint64_t at = (uint64_t)a.c.group[slab >> 1] * a.n + i;
+    const uint32_t src = (uint32_t)a.src[at], dst = (uint32_t)a.dst[at];
+    if (src >= a.c.n_pages || dst >= a.c.n_pages || src == dst) continue;
+    const uint32_t rows = a.rows ? min(a.rows[i], a.c.page_tokens) : a.c.page_tokens;
+    copy_piece(a.c, slab, src, dst, rows, piece);
+  }
+}
+
+// ---- whose pages are whose ---------------------------------------------------------
+// A pool counts each page's owners; one that has none is free. Requests are given
+// the lowest free pages, in their order: which ones does not depend on when a
+// kernel's threads run. Counts change by atomic additions, whose order does not
+// matter to their sum.
+struct PoolArgs {
+  int32_t* refs;  // [n_groups][n_pages]
+  uint32_t n_pages, n_groups, page_tokens;
+  FastDiv page;
+  uint32_t n;      // requests that want pages
+  uint32_t width;  // of a table row
+  uint8_t* status;
+  uint32_t* start;  // workspace: [n_groups][n + 1] pages that the requests before want
+  int32_t* list;    // workspace: [n_groups][n_pages] free pages, as many as are wanted
+  uint8_t* served;  // workspace: [n] status of each request
+  // tl_pages_fork
+  const int32_t* parent;
+  const int32_t* tables;  // [n_groups][n_parents][width]
+  const uint32_t* kv_len;
+  uint32_t n_parents;
+  int32_t* out_tables;  // [n_groups][n][width]; also what tl_pages_take fills
+  uint32_t* out_len;
+  // tl_pages_take
+  const uint32_t* have;
+  const uint32_t* want;
+};
+
+constexpr uint32_t kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr uint32_t kScan = 16;  // rounds of a pool's pages that are looked at together
+
+// A parent's last page, if it is partly filled and there.
+struct Fork {
+  uint32_t parent, kv, full, part;
+  bool fine;
+};
+__device__ __forceinline__ Fork fork_of(const PoolArgs& a, uint32_t r) {
+  Fork f;
+  f.parent = (uint32_t)a.parent[r];
+  f.fine = f.parent < a.n_parents;
+  f.kv = f.fine ? a.kv_len[f.parent] : 0;
+  f.full = f.kv / a.page_tokens;
+  f.part = f.kv - f.full * a.page_tokens;
+  if (f.full + (f.part ? 1 : 0) > a.width) f.fine = false;
+  return f;
+}
+__device__ __forceinline__ uint32_t last_page(const PoolArgs& a, const Fork& f, uint32_t g) {
+  return (uint32_t)a.tables[((uint64_t)g * a.n_parents + f.parent) * a.width + f.full];
+}
+
+// Entries [c0, c1) of a table row: the ones in them that name no page are wanted.
+__device__ __forceinline__ void range_of(const PoolArgs& a, uint32_t r, uint32_t& c0, uint32_t& c1, bool& fine) {
+  const uint32_t have = a.have[r], want = a.want[r], P = a.page_tokens;
+  c0 = have / P + (have % P ? 1 : 0);
+  c1 = want / P + (want % P ? 1 : 0);
+  fine = c1 <= a.width;
+  if (!fine || c1 < c0) c1 = c0;
+}
+
+__device__ __forceinline__ uint32_t lanes_below(uint64_t mask) { return __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1)); }
+
+// A lane walks its own request's range of a table row where that is short; a longer one is
+// walked by the whole wavefront, 64 entries at a time.
+constexpr uint32_t kShort = 4;
+
+// Pages that request r (a lane each) wants in group g.
+template <bool FORK>
+__device__ uint32_t wanted(const PoolArgs& a, uint32_t r, uint32_t g) {
+  if constexpr (FORK) {
+    if (r >= a.n) return 0;
+    const Fork f = fork_of(a, r);
+    return f.fine && f.part && last_page(a, f, g) < a.n_pages ? 1 : 0;
+  } else {
+    uint32_t c0 = 0, c1 = 0, n = 0;
+    bool fine = true;
+    if (r < a.n) range_of(a, r, c0, c1, fine);
+    const int32_t* row = a.out_tables + ((uint64_t)g * a.n + min(r, a.n - 1)) * a.width;
+    if (c1 - c0 <= kShort)
+      for (uint32_t c = c0; c < c1; ++c) n += row[c] < 0;
+    for (uint64_t m = __ballot(c1 - c0 > kShort); m; m &= m - 1) {
+      const uint32_t lane = (uint32_t)__builtin_ctzll(m), who = __shfl(r, lane), b0 = __shfl(c0, lane), b1 = __shfl(c1, lane);
+      const int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + who) * a.width;
+      uint32_t k = 0;
+      for (uint32_t c = b0 + (threadIdx.x & 63); c < b1; c += 64) k += theirs[c] < 0;
+      for (uint32_t d = 1; d < 64; d *= 2) k += __shfl_xor(k, d);
+      if ((threadIdx.x & 63) == lane) n = k;
+    }
+    return n;
+  }
+}
+
+// One workgroup: what every request wants, the lowest free pages, who is served;
+// tl_pages_take's entries. Some microseconds that follow each other: a step of a
+// batch asks for it once, for all layers.
+template <bool FORK>
+__global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
+  __shared__ uint32_t sums[kPlanWaves], cnt[kScan][kPlanWaves], found[TL_MAX_GROUPS];
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  for (uint32_t g = 0; g < a.n_groups; ++g) {
+    uint32_t* start = a.start + (uint64_t)g * (a.n + 1);
+    uint32_t total = 0;
+    for (uint32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
+      const uint32_t r = r0 + tid, mine = wanted<FORK>(a, r, g);
+      uint32_t incl = mine;
+      for (uint32_t k = 1; k < 64; k *= 2) {
+        const uint32_t up = __shfl_up(incl, k);
+        if (lane >= k) incl += up;
+      }
+      __syncthreads();  // the last round's sums have been read
+      if (lane == 63) sums[wave] = incl;
+      __syncthreads();
+      uint32_t before = total;
+      for (uint32_t w = 0; w < kPlanWaves; ++w) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
+      }
+      if (r < a.n) start[r] = before + incl - mine;
+    }
+    if (tid == 0) start[a.n] = total;
+    // the lowest free pages
+    const int32_t* refs = a.refs + (uint64_t)g * a.n_pages;
+    int32_t* list = a.list + (uint64_t)g * a.n_pages;
+    uint32_t have = 0;
+    for (uint64_t p0 = 0; p0 < a.n_pages && have < total; p0 += kScan * kPlanThreads) {
+      uint64_t free[kScan];
+      int32_t held[kScan];
+#pragma unroll
+      for (uint32_t k = 0; k < kScan; ++k) {
+        const uint64_t p = p0 + k * kPlanThreads + tid;
+        held[k] = p < a.n_pages ? refs[p] : 1;
+      }
+#pragma unroll
+      for (uint32_t k = 0; k < kScan; ++k) free[k] = __ballot(held[k] <= 0);
+      __syncthreads();  // the last counts have been read
+      if (lane == 0)
+#pragma unroll
+        for (uint32_t k = 0; k < kScan; ++k) cnt[k][wave] = __popcll(free[k]);
+      __syncthreads();
+#pragma unroll
+      for (uint32_t k = 0; k < kScan; ++k) {
+        uint32_t before = have;
+        for (uint32_t w = 0; w < kPlanWaves; ++w) {
+          const uint32_t c = cnt[k][w];
+          if (w < wave) before += c;
+          have += c;
+        }
+        before += lanes_below(free[k]);
+        if ((free[k] >> lane & 1) && before < total) list[before] = (int32_t)(p0 + k * kPlanThreads + tid);
+      }
+    }
+    if (tid == 0) found[g] = have;
+  }
+  __syncthreads();
+  // a request is served in all groups or in none
+  for (uint32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
+    const uint32_t r = r0 + tid;
+    uint8_t said = TL_ACCEPT;
+    uint32_t c0 = 0, c1 = 0;
+    bool fine = true;
+    if (r < a.n) {
+      if constexpr (FORK)
+        fine = fork_of(a, r).fine;
+      else
+        range_of(a, r, c0, c1, fine);
+      for (uint32_t g = 0; g < a.n_groups; ++g) {
+        const uint32_t* start = a.start + (uint64_t)g * (a.n + 1);
+        if (start[r + 1] > start[r] && start[r + 1] > found[g]) said = TL_MISSING;
+      }
+      if (!fine) said = TL_BADARG;
+      a.served[r] = said;
+      if (a.status) a.status[r] = said;
+    }
+    if constexpr (!FORK) {
+      if (said != TL_ACCEPT) c1 = c0;
+      for (uint32_t g = 0; g < a.n_groups; ++g) {
+        const int32_t* list = a.list + (uint64_t)g * a.n_pages;
+        int32_t* refs = a.refs + (uint64_t)g * a.n_pages;
+        int32_t* row = a.out_tables + ((uint64_t)g * a.n + min(r, a.n - 1)) * a.width;
+        uint32_t at = r < a.n ? a.start[(uint64_t)g * (a.n + 1) + r] : 0;
+        if (c1 - c0 <= kShort)
+          for (uint32_t c = c0; c < c1; ++c)
+            if (row[c] < 0) {
+              const int32_t p = list[at++];
+              row[c] = p;
+              refs[p] = 1;
+            }
+        for (uint64_t m = __ballot(c1 - c0 > kShort); m; m &= m - 1) {
+          const uint32_t who = (uint32_t)__builtin_ctzll(m), b0 = __shfl(c0, who), b1 = __shfl(c1, who);
+          uint32_t from = __shfl(at, who);
+          int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + __shfl(r, who)) * a.width;
+          for (uint32_t c = b0; c < b1; c += 64) {
+            const bool lacks = c + lane < b1 && theirs[c + lane] < 0;
+            const uint64_t all = __ballot(lacks);
+            if (lacks) {
+              const int32_t p = list[from + lanes_below(all)];
+              theirs[c + lane] = p;
+              refs[p] = 1;
+            }
+            from += __popcll(all);
+          }
+        }
+      }
+    }
+  }
+}
+
+struct ForkArgs {
+  Slabs c;
+  PoolArgs p;
+  uint32_t pieces;
+};
+
+// The first n * n_groups workgroups write a branch's table and count it among its
+// pages' owners; the others copy pieces of last pages.
+__global__ __launch_bounds__(kThreads) void k_pages_fork(ForkArgs a) {
+  const PoolArgs& p = a.p;
+  const uint64_t tables = (uint64_t)p.n * p.n_groups, per = (uint64_t)a.c.n_slabs * a.pieces, items = tables + p.n * per;
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    if (item < tables) {
+      const uint32_t r = (uint32_t)(item / p.n_groups), g = (uint32_t)(item % p.n_groups);
+      const bool served = p.served[r] == TL_ACCEPT;
+      const Fork f = fork_of(p, r);
+      const uint32_t* start = p.start + (uint64_t)g * (p.n + 1);
+      int32_t* refs = p.refs + (uint64_t)g * p.n_pages;
+      const bool own = served && start[r + 1] > start[r];
+      for (uint32_t c = threadIdx.x; c < p.width; c += kThreads) {
+        int32_t id = -1;
+        if (served && c < f.full) {
+          id = p.tables[((uint64_t)g * p.n_parents + f.parent) * p.width + c];
+          if ((uint32_t)id < p.n_pages)
+            atomicAdd(refs + id, 1);
+          else
+            id = -1;
+        } else if (own && c == f.full) {
+          id = p.list[(uint64_t)g * p.n_pages + start[r]];
+          refs[id] = 1;
+        }
+        p.out_tables[((uint64_t)g * p.n + r) * p.width + c] = id;
+      }
+      if (g == 0 && threadIdx.x == 0) p.out_len[r] = served ? f.kv : 0;
+      continue;
+    }
+    const uint64_t at = item - tables;
+    const uint32_t r = (uint32_t)(at / per), rest = (uint32_t)(at % per), slab = rest / a.pieces, piece = rest % a.pieces;
+    const uint32_t g = a.c.group[slab >> 1];
+    const uint32_t* start = p.start + (uint64_t)g * (p.n + 1);
+    if (p.served[r] != TL_ACCEPT || start[r + 1] == start[r]) continue;
+    const Fork f = fork_of(p, r);
+    copy_piece(a.c, slab, last_page(p, f, g), (uint32_t)p.list[(uint64_t)g * p.n_pages + start[r]], f.part, piece);
+  }
+}
+
+struct FreeArgs {
+  int32_t* refs;
+  uint32_t n_pages, page_tokens, width;
+  uint64_t rows, n;  // table rows (n for each group)
+  int32_t* tables;
+  const uint32_t* first;
+  const uint32_t* end;
+};
+
+__global__ __launch_bounds__(kThreads) void k_pages_free(FreeArgs a) {
+  const uint64_t all = a.rows * a.width;
+  for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kThreads) {
+    const uint64_t row = i / a.width;
+    const uint32_t c = (uint32_t)(i - row * a.width), r = (uint32_t)(row % a.n), P = a.page_tokens;
+    const uint32_t c0 = a.first ? a.first[r] / P + (a.first[r] % P ? 1 : 0) : 0, c1 = a.end ? a.end[r] / P : a.width;
+    if (c < c0 || c >= c1) continue;
+    const uint32_t id = (uint32_t)a.tables[i];
+    if (id < a.n_pages) atomicAdd(a.refs + row / a.n * a.n_pages + id, -1);
+    a.tables[i] = -1;
+  }
+}
+
+// ---- rows that stay --------------------------------------------------------------
+struct KeepArgs {
+  Slabs c;
+  Batch b;  // table: of group 0
+  const uint32_t* n_keep;
+  const uint32_t* keep;
+  uint32_t* len_out;
+  uint8_t* status;
+  uint32_t columns, blocks;  // 16-byte columns of a row, and workgroups that share them
+};
+
+// The smallest scale byte under which a code (not 0, without its sign) of scale byte
+// `from` is 448 or less: 1.m * 2^e needs 2^(e - 8), twice that above 1.75.
+__device__ __forceinline__ uint32_t scale_for(uint32_t code, uint32_t from) {
+  const uint32_t bits = __float_as_uint(__builtin_amdgcn_cvt_f32_fp8(code, 0));
+  const int b = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0) + (int)from;
+  return (uint32_t)max(b, (int)kScaleMin);
+}
+
+// Largest magnitude among a word's codes that are not NaN.
+__device__ __forceinline__ uint32_t largest_code(uint32_t w, uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = w >> (8 * i) & 0x7f;
+    m = c < 0x7f ? max(m, c) : m;
+  }
+  return m;
+}
+
+// Codes of scale byte `from`, rounded to scale byte `to`.
+__device__ __forceinline__ u32x4 rescale(u32x4 w, uint32_t from, uint32_t to) {
+  // 448 * 2^-40 rounds to 0, as less does; a page whose scale falls by over 2^20 holds zeros
+  const int by = min(max((int)from - (int)to, -40), 20);
+  const float f = __uint_as_float((uint32_t)(127 + by) << 23);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], true);
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * f, lo[1] * f, 0, false);
+    w[e] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * f, hi[1] * f, c, true);
+  }
+  return w;
+}
+
+// A workgroup moves C 16-byte columns of one request's rows in one slab, kRows rows
+// at a time with U more behind each. A row only moves towards the front, and never
+// past one that stays: the rows of a step are all read before the first of them is
+// written, and then no later row's source has been written over. So the request's
+// rows are moved in place, in steps that follow each other, and in parallel over
+// columns, slabs and requests.
+//
+// Scaled pages: a step is whole pages of the rows' new places, whose scales follow
+// from the codes' largest magnitudes; a page of more rows than a step holds is read
+// twice.
+template <bool FP8, int C, int U>
+struct KeepLds {
+  static constexpr uint32_t R = kThreads / C, N = R * U;  // rows at a time, rows of a step
+  int64_t from[N], to[N];                                 // bytes from a slab's start
+  uint32_t first_bad, first_move;
+  uint32_t slot[FP8 ? N : 1];               // a row's new page, among the step's
+  uint32_t need[FP8 ? N : 1][FP8 ? C / 4 : 1];  // scale bytes of those pages, of the workgroup's heads
+};
+
+template <bool FP8, int C, int U>
+__device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, uint32_t slab, uint32_t block) {
+  constexpr uint32_t R = kThreads / C, N = R * U;
+  const uint32_t tid = threadIdx.x, col = tid % C, sub = tid / C, column = block * C + col;
+  const bool there = column < a.columns;
+  const uint32_t row0 = a.b.first_row(r), row1 = a.b.first_row(r + 1), rows = row1 > row0 ? row1 - row0 : 0;
+  const uint32_t kv_len = a.b.kv_len[r], asked = a.n_keep[r], P = a.c.page_tokens;
+  const bool sound = kv_len >= rows && kv_len <= a.b.most;
+  const uint32_t before = kv_len - rows, n = sound ? min(asked, rows) : 0;
+  const uint32_t* keep = a.keep + row0;
+  const uint32_t own = a.c.group[slab >> 1];
+  const Bytes base = (Bytes)a.c.base(slab);
+  const uint64_t group_stride = (uint64_t)a.b.n_reqs * a.b.width;
+  const int32_t* table = a.b.table + (uint64_t)r * a.b.width;
+
+  // rows in front that stay where they are
+  uint32_t done = 0;
+  for (bool more = true; more && done < n;) {
+    __syncthreads();
+    if (tid == 0) l.first_move = ~0u;
+    __syncthreads();
+    const uint32_t i = done + tid;
+    if (i < n && keep[i] != i) atomicMin(&l.first_move, i);
+    __syncthreads();
+    more = l.first_move == ~0u;
+    done = more ? min(n, done + kThreads) : l.first_move;
+  }
+
+  // The places of rows [i, i + count), and how many of them can be kept: up to the
+  // first that names no later row, or has no page in some group: every layer stops
+  // at the same row.
+  uint32_t page0 = 0;  // the step's first page
+  auto find = [&](uint32_t i, uint32_t count) {
+    __syncthreads();  // what was found last has been used
+    if (tid == 0) l.first_bad = ~0u;
+    __syncthreads();
+    for (uint32_t t = tid; t < count; t += kThreads) {
+      const uint32_t k = keep[i + t], last = i + t ? keep[i + t - 1] : 0;
+      bool fine = k < rows && (i + t == 0 || k > last);
+      if (fine) {
+        const uint32_t ps = before + k, pd = before + i + t;
+        const uint32_t cs = a.b.page.div(ps), cd = a.b.page.div(pd);
+        for (uint32_t g = 0; g < a.c.n_groups; ++g) {
+          const uint32_t src = (uint32_t)table[g * group_stride + cs], dst = (uint32_t)table[g * group_stride + cd];
+          if (src >= a.c.n_pages || dst >= a.c.n_pages) fine = false;
+          if (g == own) {
+            l.from[t] = (int64_t)src * a.c.stride + (int64_t)(ps - cs * P) * a.c.row_bytes;
+            l.to[t] = (int64_t)dst * a.c.stride + (int64_t)(pd - cd * P) * a.c.row_bytes;
+          }
+        }
+        if constexpr (FP8) l.slot[t] = cd - page0;
+      }
+      if (!fine) atomicMin(&l.first_bad, t);
+    }
+    __syncthreads();
+    return min(count, l.first_bad);
+  };
+
+  bool bad = false;
+  u32x4 x[U];
+  auto load = [&](uint32_t count) {
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (there && u * R + sub < count) x[u] = *(Granules)(base + l.from[u * R + sub] + column * 16);
+  };
+  if constexpr (!FP8) {
+    while (done < n && !bad) {
+      const uint32_t ask = min(N, n - done), count = find(done, ask);
+      bad = count < ask;
+      load(count);
+      __syncthreads();  // all of the step's rows are read
+#pragma unroll
+      for (uint32_t u = 0; u < U; ++u)
+        if (there && u * R + sub < count) *(Granules)(base + l.to[u * R + sub] + column * 16) = x[u];
+      done += count;
+    }
+  } else {
+    const uint32_t lanes = a.c.row_bytes / a.c.n_scales / 16;  // of a head
+    const uint32_t head = min(column / lanes, a.c.n_scales - 1), mine = col / lanes;
+    const bool leads = there && col % lanes == 0;
+    while (done < n && !bad) {
+      const uint32_t pos = before + done;
+      page0 = a.b.page.div(pos);
+      const uint32_t o = pos - page0 * P;  // of the first page, rows before
+      const uint64_t end = ((uint64_t)page0 + (P <= N ? N / P : 1)) * P;
+      uint32_t ask = (uint32_t)min((uint64_t)(n - done), end - pos);
+      const bool whole = ask <= N;  // the rows are held, not read again
+      uint32_t scale[U];
+      auto load_scales = [&](uint32_t i, uint32_t count) {
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t t = u * R + sub;
+          if (t >= count) continue;
+          const uint32_t at = before + keep[i + t];
+          const int64_t page = l.from[t] - (int64_t)(at - a.b.page.div(at) * P) * a.c.row_bytes;
+          scale[u] = scale_held(base[page + a.c.code_bytes + head]);
+        }
+      };
+      __syncthreads();
+      for (uint32_t t = tid; t < N * (C / 4); t += kThreads) l.need[t / (C / 4)][t % (C / 4)] = kScaleMin;
+      int64_t first_page = 0;
+      for (uint32_t s = 0; s < ask; s += N) {
+        const uint32_t want = min(N, ask - s), count = find(done + s, want);
+        if (s == 0 && count) first_page = l.to[0] - (int64_t)o * a.c.row_bytes;
+        load(count);
+        load_scales(done + s, count);
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t t = u * R + sub;
+          uint32_t m = 0;
+          if (there && t < count)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = largest_code(x[u][e], m);
+          for (uint32_t k = 1; k < lanes; k *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, k));
+          if (leads && m) atomicMax(&l.need[l.slot[t]][mine], scale_for(m, scale[u]));
+        }
+        if (count < want) {
+          bad = true;
+          ask = s + count;
+        }
+      }
+      __syncthreads();  // all rows are read (or will be again), and what their pages need is known
+      if (!ask) break;
+      uint32_t first_scale = l.need[0][mine];
+      if (o) {
+        const uint32_t old = scale_held(base[first_page + a.c.code_bytes + head]);
+        if (first_scale > old) {  // the page's scale rises: the rows before are rounded again
+          for (uint32_t i = sub; i < o && there; i += R) {
+            const Granules at = (Granules)(base + first_page + (int64_t)i * a.c.row_bytes + column * 16);
+            *at = rescale(*at, old, first_scale);
+          }
+        } else {
+          first_scale = old;
+        }
+      }
+      auto store = [&](uint32_t i, uint32_t count) {
+#pragma unroll
+        for (uint32_t u = 0; u < U; ++u) {
+          const uint32_t t = u * R + sub;
+          if (!there || t >= count) continue;
+          const uint32_t to = l.slot[t] ? l.need[l.slot[t]][mine] : first_scale;
+          *(Granules)(base + l.to[t] + column * 16) = scale[u] == to ? x[u] : rescale(x[u], scale[u], to);
+          // a page's scale, with the first of its rows that move
+          if (whole && leads && (t == 0 || l.slot[t] != l.slot[t - 1])) {
+            const uint32_t at = before + i + t;
+            base[l.to[t] - (int64_t)(at - a.b.page.div(at) * P) * a.c.row_bytes + a.c.code_bytes + head] = (uint8_t)to;
+          }
+        }
+      };
+      if (whole) {
+        store(done, ask);
+      } else {
+        for (uint32_t s = 0; s < ask; s += N) {
+          const uint32_t count = min(N, ask - s);
+          find(done + s, count);
+          load(count);
+          load_scales(done + s, count);
+          __syncthreads();  // all of these rows are read
+          store(done + s, count);
+        }
+        __syncthreads();  // no row asks for the scale before any more
+        if (leads && sub == 0) base[first_page + a.c.code_bytes + head] = (uint8_t)first_scale;
+      }
+      done += ask;
+    }
+  }
+  if (slab == 0 && block == 0 && tid == 0) {
+    a.len_out[r] = sound ? before + done : kv_len;
+    if (a.status) a.status[r] = sound && !bad && asked <= rows ? TL_ACCEPT : TL_BADARG;
+  }
+}
+
+template <bool FP8, int C, int U>
+__global__ __launch_bounds__(kThreads) void k_keep(KeepArgs a) {
+  __shared__ KeepLds<FP8, C, U> l;
+  const uint64_t per = (uint64_t)a.c.n_slabs * a.blocks, items = a.b.n_reqs * per;
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t rest = (uint32_t)(item % per);
+    keep_rows<FP8, C, U>(a, l, (uint32_t)(item / per), rest / a.blocks, rest % a.blocks);
+  }
+}
+
+// ---- launching -------------------------------------------------------------------
+void fill_slabs(Slabs& s, const tl_ctx* ctx, const tl_cache* c) {
+  s.k = c->d_layer_k;
+  s.v = c->d_layer_v;
+  s.stride = c->page_stride;
+  s.n_pages = (uint32_t)c->n_pages;
+  s.n_slabs = 2 * ctx->L;
+  s.page_tokens = ctx->P;
+  const bool scaled = ctx->dtype == TL_DTYPE_FP8_SCALED;
+  s.code_bytes = scaled ? ctx->P * ctx->H * ctx->D : (uint32_t)ctx->geo.slab_bytes;
+  s.row_bytes = s.code_bytes / ctx->P;
+  s.n_scales = scaled ? ctx->H : 0;
+  s.n_groups = ctx->geo.n_groups;
+  std::copy(ctx->geo.group, ctx->geo.group + ctx->L, s.group);
+}
+
+uint32_t grid_of(uint64_t items) { return (uint32_t)std::min<uint64_t>(items, kMostGroups); }
+
+struct PoolLayout {
+  uint64_t start, list, end;
+};
+PoolLayout pool_layout(const tl_ctx* ctx, uint64_t n, uint64_t n_pages) {
+  const uint64_t G = ctx->geo.n_groups;
+  PoolLayout l;
+  l.start = (n + 255) / 256 * 256;  // behind a status for each request
+  l.list = l.start + 4 * G * (n + 1);
+  l.end = (l.list + 4 * G * n_pages + 255) / 256 * 256;
+  return l;
+}
+
+void fill_pool(PoolArgs& p, const tl_ctx* ctx, const tl_pool* pool, uint64_t n, uint64_t width, uint8_t* d_status, void* ws) {
+  const PoolLayout l = pool_layout(ctx, n, (uint64_t)pool->n_pages);
+  p.refs = pool->d_refs;
+  p.n_pages = (uint32_t)pool->n_pages;
+  p.n_groups = ctx->geo.n_groups;
+  p.page_tokens = ctx->P;
+  p.page.set(ctx->P);
+  p.n = (uint32_t)n;
+  p.width = (uint32_t)width;
+  p.status = d_status;
+  p.served = (uint8_t*)ws;
+  p.start = (uint32_t*)((uint8_t*)ws + l.start);
+  p.list = (int32_t*)((uint8_t*)ws + l.list);
+}
+
+int launched() { return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE; }
+
+}  // namespace
+
+uint64_t pages_workspace(const tl_ctx* ctx, uint64_t n, uint64_t n_pages) { return pool_layout(ctx, n, n_pages).end; }
+
+int launch_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, uint64_t n, const int32_t* d_src,
+                      const int32_t* d_dst, const uint32_t* d_rows) {
+  CopyArgs a = {};
+  fill_slabs(a.c, ctx, cache);
+  a.src = d_src;
+  a.dst = d_dst;
+  a.rows = d_rows;
+  a.n = (uint32_t)n;
+  a.pieces = pieces_of(a.c.code_bytes);
+  (void)hipGetLastError();
+  {
+    TimedLaunch timed(TL_KERNEL_PAGES, stream);
+    hipLaunchKernelGGL(k_pages_copy, dim3(grid_of((uint64_t)n * a.c.n_slabs * a.pieces)), dim3(kThreads), 0, (hipStream_t)stream, a);
+  }
+  return launched();
+}
+
+int launch_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl_cache* cache, uint64_t n_parents,
+                      const uint32_t* d_kv_len, const int32_t* d_tables, uint64_t n, const int32_t* d_parent, uint32_t* d_len_out,
+                      int32_t* d_tables_out, uint64_t width, uint8_t* d_status, void* ws) {
+  ForkArgs a = {};
+  fill_slabs(a.c, ctx, cache);
+  fill_pool(a.p, ctx, pool, n, width, d_status, ws);
+  a.p.parent = d_parent;
+  a.p.tables = d_tables;
+  a.p.kv_len = d_kv_len;
+  a.p.n_parents = (uint32_t)n_parents;
+  a.p.out_tables = d_tables_out;
+  a.p.out_len = d_len_out;
+  a.pieces = pieces_of(a.c.code_bytes);
+  hipStream_t s = (hipStream_t)stream;
+  (void)hipGetLastError();
+  {
+    TimedLaunch timed(TL_KERNEL_POOL, stream);
+    hipLaunchKernelGGL((k_pool_plan<true>), dim3(1), dim3(kPlanThreads), 0, s, a.p);
+  }
+  {
+    TimedLaunch timed(TL_KERNEL_PAGES, stream);
+    const uint64_t items = n * (a.p.n_groups + (uint64_t)a.c.n_slabs * a.pieces);
+    hipLaunchKernelGGL(k_pages_fork, dim3(grid_of(items)), dim3(kThreads), 0, s, a);
+  }
+  return launched();
+}
+
+int launch_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, uint64_t n, const uint32_t* d_have, const uint32_t* d_want,
+                      int32_t* d_tables, uint64_t width, uint8_t* d_status, void* ws) {
+  PoolArgs a = {};
+  fill_pool(a, ctx, pool, n, width, d_status, ws);
+  a.have = d_have;
+  a.want = d_want;
+  a.out_tables = d_tables;
+  (void)hipGetLastError();
+  {
+    TimedLaunch timed(TL_KERNEL_POOL, stream);
+    hipLaunchKernelGGL((k_pool_plan<false>), dim3(1), dim3(kPlanThreads), 0, (hipStream_t)stream, a);
+  }
+  return launched();
+}
+
+int launch_pages_free(const tl_ctx* ctx, void* stream, const tl_pool* pool, uint64_t n, int32_t* d_tables, uint64_t width,
+                      const uint32_t* d_first, const uint32_t* d_end) {
+  FreeArgs a = {pool->d_refs, (uint32_t)pool->n_pages, ctx->P, (uint32_t)width, n * ctx->geo.n_groups, n, d_tables, d_first, d_end};
+  (void)hipGetLastError();
+  {
+    TimedLaunch timed(TL_KERNEL_POOL, stream);
+    hipLaunchKernelGGL(k_pages_free, dim3(grid_of((a.rows * width + kThreads - 1) / kThreads)), dim3(kThreads), 0, (hipStream_t)stream, a);
+  }
+  return launched();
+}
+
+int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32_t* d_n_keep, const uint32_t* d_keep,
+                const tl_cache* cache, uint32_t* d_len_out, uint8_t* d_status) {
+  KeepArgs a = {};
+  fill_slabs(a.c, ctx, cache);
+  fill_batch(a.b, ctx, 0, batch);
+  a.b.table = batch->d_tables;
+  a.n_keep = d_n_keep;
+  a.keep = d_keep;
+  a.len_out = d_len_out;
+  a.status = d_status;
+  a.columns = a.c.row_bytes / 16;
+  const bool many = batch->n_rows / batch->n_reqs > 256;
+  const uint32_t C = many ? 16 : 64;
+  a.blocks = (a.columns + C - 1) / C;
+  const dim3 grid(grid_of((uint64_t)batch->n_reqs * a.c.n_slabs * a.blocks));
+  hipStream_t s = (hipStream_t)stream;
+  (void)hipGetLastError();
+  {
+    TimedLaunch timed(TL_KERNEL_KEEP, stream);
+    if (ctx->dtype == TL_DTYPE_FP8_SCALED) {
+      if (many)
+        hipLaunchKernelGGL((k_keep<true, 16, 8>), grid, dim3(kThreads), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_keep<true, 64, 4>), grid, dim3(kThreads), 0, s, a);
+    } else {
+      if (many)
+        hipLaunchKernelGGL((k_keep<false, 16, 8>), grid, dim3(kThreads), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_keep<false, 64, 4>), grid, dim3(kThreads), 0, s, a);
+    }
+  }
+  return launched();
+}
+
+}  // namespace tl

@@ -81,6 +81,10 @@ class tl_rope(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
+class tl_pool(ctypes.Structure):
+    _fields_ = [("d_refs", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
+
+
 # torch's types of the operators' arguments, where torch is there
 _BF16 = None
 _WORDS = _FLOATS = _BYTES = ()
@@ -141,6 +145,13 @@ def _load():
         "tl_attend_workspace_bytes": (c.c_size_t, [P, c.c_uint32, c.c_size_t, c.c_size_t]),
         "tl_attend": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.c_uint32, c.POINTER(tl_rows),
                                 c.POINTER(tl_cache), c.c_float, c.c_uint32, c.POINTER(tl_rows), P, P, c.c_size_t]),
+        "tl_pages_copy": (c.c_int, [P, P, c.POINTER(tl_cache), c.c_size_t, P, P, P]),
+        "tl_pages_fork": (c.c_int, [P, P, c.POINTER(tl_pool), c.POINTER(tl_cache), c.c_size_t, P, P, c.c_size_t, P, P, P,
+                                    c.c_size_t, P, P, c.c_size_t]),
+        "tl_pages_take": (c.c_int, [P, P, c.POINTER(tl_pool), c.c_size_t, P, P, P, c.c_size_t, P, P, c.c_size_t]),
+        "tl_pages_free": (c.c_int, [P, P, c.POINTER(tl_pool), c.c_size_t, P, c.c_size_t, P, P]),
+        "tl_pages_workspace_bytes": (c.c_size_t, [P, c.c_size_t, c.c_size_t]),
+        "tl_keep": (c.c_int, [P, P, c.POINTER(tl_batch), P, P, c.POINTER(tl_cache), P, P]),
         "tl_file_open": (P, [c.c_char_p, c.c_uint64, c.c_int, c.c_int, c.POINTER(c.c_int)]),
         "tl_file_close": (c.c_int, [P]),
         "tl_file_records": (c.c_uint64, [P]),
@@ -170,12 +181,14 @@ EXPORTED = (
     "tl_dindex_bytes", "tl_dindex_create", "tl_dindex_destroy", "tl_dindex_workspace_bytes",
     "tl_dindex_put", "tl_dindex_get", "tl_dindex_stats", "tl_chain_lookup", "tl_chain_stage",
     "tl_block_fingerprints", "tl_chain_lookup_par", "tl_append", "tl_attend_workspace_bytes", "tl_attend",
+    "tl_pages_copy", "tl_pages_fork", "tl_pages_take", "tl_pages_free", "tl_pages_workspace_bytes", "tl_keep",
     "tl_file_open", "tl_file_close", "tl_file_records",
     "tl_file_read", "tl_file_write", "tl_file_drop_cache",
     "tl_status_string", "tl_verdict_string", "tl_abi_version", "tl_test_sha256", "tl_timing",
     "tl_timing_read")
 KERNELS = {"save_seg": 0, "save_meta": 1, "load_init": 2, "load_main": 3, "load_final": 4, "chain": 5,
-           "stage": 6, "index": 7, "append": 8, "attend": 9, "attend_join": 10}
+           "stage": 6, "index": 7, "append": 8, "attend": 9, "attend_join": 10,
+           "pages": 11, "pool": 12, "keep": 13}
 TL_INDEX_STORED, TL_INDEX_FULL, TL_INDEX_TAG_CLASH = 0x01, 0x20, 0x21
 TL_CHAIN_ALL_KEYS, TL_CHAIN_TAIL = 1, 2
 TL_KEYS_TAIL = 1
@@ -689,6 +702,99 @@ def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q,
                         _rows(out, n, dim, "results"), _addr(lse), _addr(d_workspace), workspace_bytes)
     if st:
         _check(st, "tl_attend")
+
+
+# ------------------------------------------------------------------ pages of a cache
+def make_pool(d_refs, n_pages: Optional[int] = None) -> tl_pool:
+    """Owners of each page (tl_pool): i32 [n_groups, n_pages] on the device; 0: free."""
+    _of_type(d_refs, _WORDS, "page counts")
+    n_pages = d_refs.shape[-1] if n_pages is None else n_pages
+    _fits(d_refs, 4 * n_pages, "page counts")
+    p = tl_pool(_addr(d_refs), n_pages)
+    p._keep = (d_refs,)
+    return p
+
+
+def _check_pool(ctx: Ctx, pool: tl_pool):
+    keep = getattr(pool, "_keep", None)
+    if keep is not None:
+        _fits(keep[0], 4 * ctx.n_groups * pool.n_pages, "page counts")
+
+
+def _words(x, n: int, what: str):
+    _of_type(x, _WORDS, what)
+    _fits(x, 4 * n, what)
+    return _addr(x)
+
+
+def _status(x, n: int):
+    _of_type(x, _BYTES, "status")
+    _fits(x, n, "status")
+    return _addr(x)
+
+
+def tl_pages_copy(ctx: Ctx, stream, cache: tl_cache, n: int, d_src, d_dst, d_rows=None):
+    """Copies the first d_rows[i] tokens (None: all) of page d_src[g, i] to page
+    d_dst[g, i], i < n, in every layer of each group g."""
+    _check_cache(ctx, cache)
+    st = _lib.tl_pages_copy(ctx.handle, _stream(stream), cache, n, _words(d_src, ctx.n_groups * n, "source pages"),
+                            _words(d_dst, ctx.n_groups * n, "destination pages"), _words(d_rows, n, "rows"))
+    if st:
+        _check(st, "tl_pages_copy")
+
+
+def tl_pages_workspace_bytes(ctx: Ctx, n: int, n_pages: int) -> int:
+    return int(_lib.tl_pages_workspace_bytes(ctx.handle, n, n_pages))
+
+
+def tl_pages_fork(ctx: Ctx, stream, pool: tl_pool, cache: tl_cache, n_parents: int, d_kv_len, d_tables, n: int, d_parent, d_len_out,
+                  d_tables_out, table_width: int, d_workspace, workspace_bytes: int, d_status=None):
+    """n branches of the requests d_tables [n_groups, n_parents, table_width]: branch i
+    continues request d_parent[i] on the pages of d_tables_out [n_groups, n, table_width]."""
+    _check_cache(ctx, cache)
+    _check_pool(ctx, pool)
+    _fits(d_workspace, workspace_bytes, "workspace")
+    row = ctx.n_groups * table_width
+    st = _lib.tl_pages_fork(ctx.handle, _stream(stream), pool, cache, n_parents, _words(d_kv_len, n_parents, "cache lengths"),
+                            _words(d_tables, row * n_parents, "page tables"), n, _words(d_parent, n, "parents"),
+                            _words(d_len_out, n, "branches' lengths"), _words(d_tables_out, row * n, "branches' page tables"),
+                            table_width, _status(d_status, n), _addr(d_workspace), workspace_bytes)
+    if st:
+        _check(st, "tl_pages_fork")
+
+
+def tl_pages_take(ctx: Ctx, stream, pool: tl_pool, n: int, d_have, d_want, d_tables, table_width: int, d_workspace,
+                  workspace_bytes: int, d_status=None):
+    """Free pages for the tokens [d_have[i], d_want[i]) of n requests, into d_tables
+    [n_groups, n, table_width]."""
+    _check_pool(ctx, pool)
+    _fits(d_workspace, workspace_bytes, "workspace")
+    st = _lib.tl_pages_take(ctx.handle, _stream(stream), pool, n, _words(d_have, n, "lengths"), _words(d_want, n, "lengths"),
+                            _words(d_tables, ctx.n_groups * n * table_width, "page tables"), table_width, _status(d_status, n),
+                            _addr(d_workspace), workspace_bytes)
+    if st:
+        _check(st, "tl_pages_take")
+
+
+def tl_pages_free(ctx: Ctx, stream, pool: tl_pool, n: int, d_tables, table_width: int, d_first=None, d_end=None):
+    """Gives back the pages that d_tables [n_groups, n, table_width] names within tokens
+    [d_first[i], d_end[i]) (None: from the first; to the row's end)."""
+    _check_pool(ctx, pool)
+    st = _lib.tl_pages_free(ctx.handle, _stream(stream), pool, n, _words(d_tables, ctx.n_groups * n * table_width, "page tables"),
+                            table_width, _words(d_first, n, "first tokens"), _words(d_end, n, "ends"))
+    if st:
+        _check(st, "tl_pages_free")
+
+
+def tl_keep(ctx: Ctx, stream, batch: tl_batch, cache: tl_cache, d_n_keep, d_keep, d_len_out, d_status=None):
+    """Moves the new tokens that stay together, in every layer: request r's new token
+    d_keep[d_row_off[r] + i] becomes its new token i, i < d_n_keep[r]."""
+    _check_operator(ctx, batch, cache)
+    n = batch.n_reqs
+    st = _lib.tl_keep(ctx.handle, _stream(stream), batch, _words(d_n_keep, n, "counts"), _words(d_keep, batch.n_rows, "kept rows"), cache,
+                      _words(d_len_out, n, "new lengths"), _status(d_status, n))
+    if st:
+        _check(st, "tl_keep")
 
 
 # ------------------------------------------------------------------ record files (disk tier)
