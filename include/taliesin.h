@@ -561,6 +561,24 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
               const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
               const tl_cache* cache, uint8_t* d_status);
 
+/* tl_append for models that norm each head of the queries and keys before they are
+ * rotated: a head x of head_dim elements becomes x / sqrt(mean(x^2) + eps) times its
+ * weights, with TL_NORM_CENTER less its mean first, in 32-bit arithmetic; nothing is
+ * rounded to 16 bits between the norm and the rotation. Values are not normed. norm NULL:
+ * tl_append. */
+#define TL_NORM_CENTER 1
+typedef struct tl_norm {
+  const float* d_q_weight; /* device, 16-byte aligned: head h's head_dim weights begin at   */
+  const float* d_k_weight; /* d_q_weight + h * q_stride (K heads: k_stride); NULL: all 1    */
+  int64_t q_stride;        /* elements, multiples of 4; 0: the same weights for all heads   */
+  int64_t k_stride;
+  float eps;               /* at least FLT_MIN */
+  uint32_t flags;          /* 0 or TL_NORM_CENTER */
+} tl_norm;
+int tl_append_norm(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_norm* norm,
+                   const tl_rope* rope, const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q,
+                   const tl_rows* q_out, const tl_cache* cache, uint8_t* d_status);
+
 /* Attention of every row over its request's cached keys and values:
  * out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale * q . k_j), over the keys
  * j at positions up to the row's own, and above its own minus the layer's window

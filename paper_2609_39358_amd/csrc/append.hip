@@ -1,5 +1,5 @@
-// tl_append: the new tokens' keys and values into the pages of a cache, keys and
-// queries rotated on the way.
+// tl_append, tl_append_norm: the new tokens' keys and values into the pages of a cache,
+// keys and queries normed and rotated on the way.
 #include <algorithm>
 
 #include "paged.h"
@@ -26,6 +26,11 @@ struct AppendArgs {
   const f32x2* cos_sin;  // [n_angles][rot / 2]
   const int32_t* pos;    // [n_axes][n_rows], or null: a token's place in its request
   uint32_t axis[8];      // two bits per pair
+  // norms of queries (0) and keys (1): weights of a head, or null for ones
+  const float* weight[2];
+  int64_t weight_head[2];  // elements from one head's to the next's; 0: all heads' are the same
+  float eps;
+  uint32_t center;  // the mean is taken off first
   uint8_t* status;
   // the first part of the grid, with scaled pages
   uint32_t n_windows, step;  // windows of so many rows
@@ -136,11 +141,88 @@ __device__ __forceinline__ void rotate(const AppendArgs& a, uint32_t j, const An
   }
 }
 
-// Lane j's 16 elements of a row, as they were read, turned by the row's angles; a
-// row that has none is kept as zeros, and reported.
-__device__ __forceinline__ void values(const AppendArgs& a, const u32x4* raw, bool turned, uint32_t j, const Angles& g, float* x) {
+// The sum over a row's lanes, the same on all of them.
+template <int D>
+__device__ __forceinline__ float row_sum(float s) {
+#pragma unroll
+  for (int k = 1; k < Row<D>::kLanes; k *= 2) s += __shfl_xor(s, k);
+  return s;
+}
+
+// x / sqrt(mean(x^2) + eps) of a row of D elements, less its mean first where that is
+// asked for (the mean before the squares: no difference of large sums). In 32 bits; each
+// operation is rounded by itself, as in turn().
+template <int D>
+__device__ __forceinline__ float centered_squares(bool center, float* x) {
+#pragma clang fp contract(off)
+  if (center) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += x[i];
+    s = row_sum<D>(s) * (1.f / D);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] -= s;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += x[i] * x[i];
+  return row_sum<D>(s) * (1.f / D);
+}
+template <int D>
+__device__ __forceinline__ void norm(const AppendArgs& a, float* x) {
+#pragma clang fp contract(off)
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = x[i];
+  float s = centered_squares<D>(a.center, y);
+  float eps = a.eps;
+  if (!(s < __uint_as_float(kInfinite))) {
+    // Values of 2^60 and more: their squares pass 32 bits, but not those of 2^-70 times
+    // them (and values that are not finite stay what they are).
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i] * 0x1p-70f;
+    s = centered_squares<D>(a.center, y);
+    eps = 0.f;
+  }
+  const float r = 1.f / __builtin_sqrtf(s + eps);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = y[i] * r;
+}
+
+// Lane j's weights of a head (of queries 0, of keys 1), at the elements that it holds.
+struct Weights {
+  f32x4 w[4];
+};
+__device__ __forceinline__ Weights load_weights(const AppendArgs& a, int which, uint32_t head, uint32_t first, uint32_t second) {
+  Weights y;
+  const float* p = a.weight[which];
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y.w[i] = f32x4{1.f, 1.f, 1.f, 1.f};
+    return y;
+  }
+  p += (int64_t)head * a.weight_head[which];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    y.w[i] = *(const f32x4*)(p + first + 4 * i);
+    y.w[2 + i] = *(const f32x4*)(p + second + 4 * i);
+  }
+  return y;
+}
+
+// Lane j's 16 elements of a row, as they were read, normed (w) and turned by the row's
+// angles; a row that has none is kept as zeros, and reported.
+template <int D, bool NORM>
+__device__ __forceinline__ void values(const AppendArgs& a, const u32x4* raw, bool turned, uint32_t j, const Angles& g, const Weights* w, float* x) {
   unpack(raw[0], x);
   unpack(raw[1], x + 8);
+  if constexpr (NORM) {
+    if (turned) {
+      norm<D>(a, x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] *= w->w[i / 4][i % 4];
+    }
+  }
   if (!g.ok) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
@@ -196,7 +278,7 @@ struct Shared {
 // scale is known; with fewer tokens it takes several heads, and up to all four
 // share the tokens of one. Of more tokens than four can hold the earlier ones are
 // read again.
-template <int D, int HELD>
+template <int D, int HELD, bool NORM>
 __device__ void put_fragment(const AppendArgs& a, Shared& l, uint32_t head0, uint32_t head1, uint32_t r, uint32_t t, uint32_t n,
                              int64_t position) {
   constexpr int L = Row<D>::kLanes, R = Row<D>::kRows;
@@ -213,6 +295,7 @@ __device__ void put_fragment(const AppendArgs& a, Shared& l, uint32_t head0, uin
   Angles g[HELD];
   u32x4 raw[2][HELD][2];
   float x[2][HELD][16];
+  Weights weights;
   auto angles = [&](uint32_t c) {
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
@@ -221,6 +304,7 @@ __device__ void put_fragment(const AppendArgs& a, Shared& l, uint32_t head0, uin
     }
   };
   auto load = [&](uint32_t head, uint32_t c) {
+    if constexpr (NORM) weights = load_weights(a, 1, min(head, head1 - 1), first[0], second[0]);
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
       const uint32_t i = min(c * chunk + h * every + sub, n - 1);
@@ -235,8 +319,8 @@ __device__ void put_fragment(const AppendArgs& a, Shared& l, uint32_t head0, uin
   auto convert = [&] {
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
-      values(a, raw[0][h], true, j, g[h], x[0][h]);
-      values(a, raw[1][h], false, j, g[h], x[1][h]);
+      values<D, NORM>(a, raw[0][h], true, j, g[h], &weights, x[0][h]);
+      values<D, NORM>(a, raw[1][h], false, j, g[h], nullptr, x[1][h]);
     }
   };
 
@@ -349,7 +433,7 @@ __device__ void put_fragment(const AppendArgs& a, Shared& l, uint32_t head0, uin
 
 // A wavefront's row t: its status, its queries, and with bf16 pages its K and V.
 // They are lines of D elements that the same angles turn.
-template <int D, bool FP8>
+template <int D, bool FP8, bool NORM>
 __device__ void put_row(const AppendArgs& a, uint32_t t) {
   constexpr int L = Row<D>::kLanes, R = Row<D>::kRows, kBatch = 4;
   const uint32_t lane = threadIdx.x & 63, j = lane % L, H = a.n_heads, nq = a.q.p ? a.n_q_heads : 0;
@@ -398,7 +482,10 @@ __device__ void put_row(const AppendArgs& a, uint32_t t) {
       if (u >= lines) continue;
       const bool is_v = !FP8 && u >= nq + H;
       float x[16];
-      values(a, raw[i], !is_v, j, g, x);
+      Weights w;
+      if constexpr (NORM)
+        if (!is_v) w = load_weights(a, u >= nq, u >= nq ? u - nq : u, first, second);
+      values<D, NORM>(a, raw[i], !is_v, j, g, &w, x);
       GlobalOut out = (GlobalOut)(a.q_out + (int64_t)t * a.qo_token + (int64_t)u * a.qo_head);
       if (!FP8 && u >= nq) {
         if (!has_place) continue;
@@ -413,7 +500,7 @@ __device__ void put_row(const AppendArgs& a, uint32_t t) {
 // The first n_windows * splits workgroups take a window of `step` rows and some heads
 // of K and V each: those fragments (rows of one request that go to one scaled page)
 // that begin there. The others take a row per wavefront.
-template <int D, int HELD>
+template <int D, int HELD, bool NORM>
 __global__ __launch_bounds__(64 * kWaves) void k_append(AppendArgs a) {
   constexpr bool FP8 = HELD > 0;
   uint32_t block = blockIdx.x;
@@ -444,7 +531,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_append(AppendArgs a) {
         }
         if (t == row0 || o == 0) {
           __syncthreads();  // what the last fragment shared has been read
-          put_fragment<D, HELD>(a, l, head0, head1, r, t, n, position);
+          put_fragment<D, HELD, NORM>(a, l, head0, head1, r, t, n, position);
         }
         t += n;
       }
@@ -453,21 +540,21 @@ __global__ __launch_bounds__(64 * kWaves) void k_append(AppendArgs a) {
     block -= a.n_windows * a.splits;
   }
   const uint32_t t = block * kWaves + threadIdx.x / 64;
-  if (t < a.b.n_rows) put_row<D, FP8>(a, t);
+  if (t < a.b.n_rows) put_row<D, FP8, NORM>(a, t);
 }
 
-template <int D>
+template <int D, bool NORM>
 void launch(bool fp8, uint32_t grid, hipStream_t s, const AppendArgs& a) {
   if (!fp8)
-    hipLaunchKernelGGL((k_append<D, 0>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((k_append<D, 0, NORM>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   else if (a.step <= (uint32_t)Row<D>::kRows || (a.n_windows >= 256 && a.step <= (uint32_t)(kWaves * Row<D>::kRows)))
     // A lane holds one row: where one wavefront's lanes hold a window, or, with many
     // windows, four do. 24,573 tokens into pages of 16 rows of 16 heads of 128: 153 us,
     // 4.7 TB/s, with two rows held 170; 64 requests of 2 rows 7.6 and 9.5; 128
     // windows of 16 rows 17.7 and 14.9.
-    hipLaunchKernelGGL((k_append<D, 1>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((k_append<D, 1, NORM>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   else
-    hipLaunchKernelGGL((k_append<D, 2>), dim3(grid), dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((k_append<D, 2, NORM>), dim3(grid), dim3(64 * kWaves), 0, s, a);
 }
 
 }  // namespace
@@ -492,7 +579,7 @@ void fill_pages(Pages& p, const tl_ctx* ctx, uint32_t layer, const tl_cache* c) 
   p.scale_off = ctx->P * ctx->H * ctx->D;
 }
 
-int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
+int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_norm* norm, const tl_rope* rope,
                   const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
                   const tl_cache* cache, uint8_t* d_status) {
   AppendArgs a = {};
@@ -519,6 +606,14 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     a.pos = rope->d_pos;
     for (uint32_t i = 0; rope->pair_axis && i < rope->rot_dim / 2; ++i)
       a.axis[i >> 4] |= (uint32_t)rope->pair_axis[i] << (2 * (i & 15));
+  }
+  if (norm) {
+    a.weight[0] = norm->d_q_weight;
+    a.weight[1] = norm->d_k_weight;
+    a.weight_head[0] = norm->q_stride;
+    a.weight_head[1] = norm->k_stride;
+    a.eps = norm->eps;
+    a.center = (norm->flags & TL_NORM_CENTER) != 0;
   }
   a.status = d_status;
   const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED;
@@ -547,11 +642,11 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
   {
     TimedLaunch timed(TL_KERNEL_APPEND, stream);
     if (ctx->D == 64)
-      launch<64>(fp8, grid, s, a);
+      norm ? launch<64, true>(fp8, grid, s, a) : launch<64, false>(fp8, grid, s, a);
     else if (ctx->D == 128)
-      launch<128>(fp8, grid, s, a);
+      norm ? launch<128, true>(fp8, grid, s, a) : launch<128, false>(fp8, grid, s, a);
     else
-      launch<256>(fp8, grid, s, a);
+      norm ? launch<256, true>(fp8, grid, s, a) : launch<256, false>(fp8, grid, s, a);
   }
   return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE;
 }

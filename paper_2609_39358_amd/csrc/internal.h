@@ -111,7 +111,7 @@ int launch_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_chai
                  const int32_t* d_tables_in, int32_t* d_tables_out);
 
 // The operators on a paged cache; append.hip, attend.hip.
-int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
+int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_norm* norm, const tl_rope* rope,
                   const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
                   const tl_cache* cache, uint8_t* d_status);
 // Bytes of workspace of one call, and of any call with at most so many rows.

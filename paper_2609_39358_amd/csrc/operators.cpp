@@ -1,5 +1,6 @@
 // Argument validation of the operators on a paged cache (tl_append, tl_attend,
 // tl_pages_*, tl_keep), in front of their launches.
+#include <float.h>
 #include <math.h>
 
 #include "internal.h"
@@ -81,6 +82,9 @@ bool result_ok(const tl_rows* r, uint64_t n_rows, uint32_t n_heads, uint32_t dim
   return rows_outside || heads_outside;
 }
 
+// Weights of a norm are read 16 bytes at a time.
+bool weights_ok(int64_t stride) { return stride % 4 == 0 && stride >= -(1ll << 40) && stride <= 1ll << 40; }
+
 bool heads_ok(const tl_ctx* ctx, uint32_t n_q_heads) {
   return n_q_heads && n_q_heads % ctx->H == 0 && n_q_heads <= kMaxHeads;
 }
@@ -92,11 +96,22 @@ extern "C" {
 int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_rope* rope,
               const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
               const tl_cache* cache, uint8_t* d_status) {
+  return tl_append_norm(ctx, stream, layer, batch, nullptr, rope, k, v, n_q_heads, q, q_out, cache, d_status);
+}
+
+int tl_append_norm(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_norm* norm,
+                   const tl_rope* rope, const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q,
+                   const tl_rows* q_out, const tl_cache* cache, uint8_t* d_status) {
   if (!ctx) return TL_EINVAL;
   int r = check_layer(ctx, layer, cache);
   if (r) return r;
   if ((r = check_batch(batch))) return r;
   if (!q != !q_out || !q != !n_q_heads || n_q_heads > kMaxHeads) return TL_EINVAL;
+  if (norm) {
+    if (!(norm->eps >= FLT_MIN) || !isfinite(norm->eps) || (norm->flags & ~uint32_t(TL_NORM_CENTER))) return TL_EINVAL;
+    if (((uintptr_t)norm->d_q_weight | (uintptr_t)norm->d_k_weight) & 15) return TL_EINVAL;
+    if (!weights_ok(norm->q_stride) || !weights_ok(norm->k_stride)) return TL_EINVAL;
+  }
   if (rope) {
     if (rope->rot_dim > ctx->D || rope->rot_dim % 16 || !rope->rot_dim) return TL_EINVAL;
     if (!rope->d_cos_sin || ((uintptr_t)rope->d_cos_sin & 15) || rope->n_angles < 1) return TL_EINVAL;
@@ -115,7 +130,7 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
     if (q->d_rows == q_out->d_rows && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
       return TL_EINVAL;
   }
-  return tl::launch_append(ctx, stream, layer, batch, rope, k, v, n_q_heads, q, q_out, cache, d_status);
+  return tl::launch_append(ctx, stream, layer, batch, norm, rope, k, v, n_q_heads, q, q_out, cache, d_status);
 }
 
 size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t /*n_reqs*/, size_t n_rows) {

@@ -81,6 +81,11 @@ class tl_rope(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
+class tl_norm(ctypes.Structure):
+    _fields_ = [("d_q_weight", ctypes.c_void_p), ("d_k_weight", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
 class tl_pool(ctypes.Structure):
     _fields_ = [("d_refs", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
 
@@ -142,6 +147,9 @@ def _load():
         "tl_append": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.POINTER(tl_rope), c.POINTER(tl_rows),
                                 c.POINTER(tl_rows), c.c_uint32, c.POINTER(tl_rows), c.POINTER(tl_rows),
                                 c.POINTER(tl_cache), P]),
+        "tl_append_norm": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.POINTER(tl_norm), c.POINTER(tl_rope),
+                                     c.POINTER(tl_rows), c.POINTER(tl_rows), c.c_uint32, c.POINTER(tl_rows),
+                                     c.POINTER(tl_rows), c.POINTER(tl_cache), P]),
         "tl_attend_workspace_bytes": (c.c_size_t, [P, c.c_uint32, c.c_size_t, c.c_size_t]),
         "tl_attend": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.c_uint32, c.POINTER(tl_rows),
                                 c.POINTER(tl_cache), c.c_float, c.c_uint32, c.POINTER(tl_rows), P, P, c.c_size_t]),
@@ -180,7 +188,8 @@ EXPORTED = (
     "tl_index_destroy", "tl_index_put", "tl_index_get_batch", "tl_index_size", "tl_index_lookup_prefix",
     "tl_dindex_bytes", "tl_dindex_create", "tl_dindex_destroy", "tl_dindex_workspace_bytes",
     "tl_dindex_put", "tl_dindex_get", "tl_dindex_stats", "tl_chain_lookup", "tl_chain_stage",
-    "tl_block_fingerprints", "tl_chain_lookup_par", "tl_append", "tl_attend_workspace_bytes", "tl_attend",
+    "tl_block_fingerprints", "tl_chain_lookup_par", "tl_append", "tl_append_norm", "tl_attend_workspace_bytes",
+    "tl_attend",
     "tl_pages_copy", "tl_pages_fork", "tl_pages_take", "tl_pages_free", "tl_pages_workspace_bytes", "tl_keep",
     "tl_file_open", "tl_file_close", "tl_file_records",
     "tl_file_read", "tl_file_write", "tl_file_drop_cache",
@@ -591,6 +600,7 @@ def tl_chain_stage(ctx: Ctx, stream, n_chains: int, chains: tl_chains, d_hits, d
 
 # ------------------------------------------------------------------ operators on the paged cache
 TL_ROPE_ADJACENT = 1
+TL_NORM_CENTER = 1
 TL_ATTEND_ALL = 1
 
 
@@ -636,6 +646,28 @@ def make_rope(d_cos_sin, rot_dim: int, d_pos=None, pair_axis: Optional[Sequence[
     return r
 
 
+def make_norm(d_q_weight, d_k_weight, eps: float = 1e-6, center: bool = False) -> tl_norm:
+    """Norms of queries and keys (tl_norm): f32 weights [head_dim] for all heads, or
+    [heads, head_dim], or None for ones; center: the mean is taken off first."""
+    for x in (d_q_weight, d_k_weight):
+        if x is None:
+            continue
+        _of_type(x, _FLOATS, "norm weights")
+        if x.dim() not in (1, 2):
+            raise ValueError("norm weights have shape %s" % (tuple(x.shape),))
+        _fits(x, 0, "norm weights")
+    by = [0 if x is None or x.dim() == 1 else x.shape[1] for x in (d_q_weight, d_k_weight)]
+    n = tl_norm(_addr(d_q_weight), _addr(d_k_weight), by[0], by[1], eps, TL_NORM_CENTER if center else 0)
+    n._keep = (d_q_weight, d_k_weight)
+    return n
+
+
+def _check_norm(norm: tl_norm, dim: int, heads: Sequence[int]):
+    for x, n in zip(getattr(norm, "_keep", ()), heads):
+        if x is not None and n and (x.shape[-1] != dim or (x.dim() == 2 and x.shape[0] != n)):
+            raise ValueError("norm weights %s for %d heads of %d" % (tuple(x.shape), n, dim))
+
+
 def _rows(x, n_rows: int, dim: int, what: str) -> tl_rows:
     """A bf16 device tensor [n_rows, heads, head_dim] whose last dimension is
     contiguous; any other strides that are multiples of 8."""
@@ -659,9 +691,10 @@ def _check_operator(ctx: Ctx, batch: tl_batch, cache: tl_cache):
 
 
 def tl_append(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, k, v, rope: Optional[tl_rope] = None,
-              q=None, q_out=None, d_status=None):
+              q=None, q_out=None, d_status=None, norm: Optional[tl_norm] = None):
     """Rotates and appends the rows' keys and values [n_rows, n_kv_heads,
-    head_dim] to the cache's pages, and rotates the queries q into q_out."""
+    head_dim] to the cache's pages, and rotates the queries q into q_out; with a
+    norm, keys and queries are normed before (tl_append_norm)."""
     _check_operator(ctx, batch, cache)
     n, dim, heads = batch.n_rows, ctx.head_dim, 0
     if k.shape[1] != ctx.n_kv_heads or v.shape[1] != ctx.n_kv_heads:
@@ -676,10 +709,14 @@ def tl_append(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, k,
         keep = getattr(rope, "_keep", None)
         if keep is not None and keep[1] is not None:
             _fits(keep[1], 4 * rope.n_axes * n, "positions")
-    st = _lib.tl_append(ctx.handle, _stream(stream), layer, batch, rope, _rows(k, n, dim, "keys"), _rows(v, n, dim, "values"),
-                        heads, q, q_out, cache, _addr(d_status))
+    k, v = _rows(k, n, dim, "keys"), _rows(v, n, dim, "values")
+    if norm is None:
+        st = _lib.tl_append(ctx.handle, _stream(stream), layer, batch, rope, k, v, heads, q, q_out, cache, _addr(d_status))
+    else:
+        _check_norm(norm, dim, (heads, ctx.n_kv_heads))
+        st = _lib.tl_append_norm(ctx.handle, _stream(stream), layer, batch, norm, rope, k, v, heads, q, q_out, cache, _addr(d_status))
     if st:
-        _check(st, "tl_append")
+        _check(st, "tl_append" if norm is None else "tl_append_norm")
 
 
 def tl_attend_workspace_bytes(ctx: Ctx, n_q_heads: int, n_reqs: int, n_rows: int) -> int:
