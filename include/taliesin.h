@@ -602,6 +602,26 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
               const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
               float* d_lse, void* d_workspace, size_t workspace_bytes);
 
+/* Attention of drafted tokens, whose new rows are not one text but a tree: row t sees its
+ * request's cached keys before the new tokens (all of them, or where the layer has a
+ * window those above its own position minus the window), and of the new tokens those that
+ * its mask names: new token i (batch row d_row_off[r] + i) by bit i % 64 of word i / 64;
+ * tokens past the mask's words are not seen. A row sees itself only if its mask says so,
+ * and the masks alone decide about new tokens, whatever their positions. In all else
+ * tl_attend: results, d_lse, rows that see nothing, missing pages, values that are not
+ * finite, workspace (tl_attend_workspace_bytes) and kernels. The rows are appended in the
+ * tree's order with their depths as positions (tl_rope.d_pos); after a choice of tokens
+ * tl_keep moves those that stay together. */
+typedef struct tl_tree {
+  const uint64_t* d_seen; /* device [n_rows][words] */
+  const int32_t* d_pos;   /* device [n_rows] positions in the request, for layers with a window
+                             (else it may be NULL); taken to lie among the new tokens' places */
+  uint32_t words;         /* at least 1, at most 2^18 */
+} tl_tree;
+int tl_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_tree* tree,
+                   uint32_t n_q_heads, const tl_rows* q, const tl_cache* cache, float scale, const tl_rows* out,
+                   float* d_lse, void* d_workspace, size_t workspace_bytes);
+
 /* ---- pages of a cache ---------------------------------------------------------
  * Requests that branch (several answers to one prompt, beams) share the pages that
  * they have in common. These calls work on whole pages of every layer at once, of

@@ -110,7 +110,7 @@ int launch_stage(const tl_ctx* ctx, void* stream, size_t n_chains, const tl_chai
                  uint64_t* d_bidx, uint32_t* d_tokens_out, uint32_t* d_n_tokens_out,
                  const int32_t* d_tables_in, int32_t* d_tables_out);
 
-// The operators on a paged cache; append.hip, attend.hip.
+// The operators on a paged cache; append.hip, attend.hip, attend_tree.hip.
 int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_norm* norm, const tl_rope* rope,
                   const tl_rows* k, const tl_rows* v, uint32_t n_q_heads, const tl_rows* q, const tl_rows* q_out,
                   const tl_cache* cache, uint8_t* d_status);
@@ -120,6 +120,8 @@ size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_rows);
 int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
                   const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
                   float* d_lse, void* d_ws);
+int launch_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_tree* tree, uint32_t n_q_heads,
+                       const tl_rows* q, const tl_cache* cache, float scale, const tl_rows* out, float* d_lse, void* d_ws);
 
 // Pages as a whole; pages.hip.
 uint64_t pages_workspace(const tl_ctx* ctx, uint64_t n, uint64_t n_pages);

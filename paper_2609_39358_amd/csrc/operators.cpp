@@ -1,5 +1,5 @@
-// Argument validation of the operators on a paged cache (tl_append, tl_attend,
-// tl_pages_*, tl_keep), in front of their launches.
+// Argument validation of the operators on a paged cache (tl_append, tl_attend
+// and their variants, tl_pages_*, tl_keep), in front of their launches.
 #include <float.h>
 #include <math.h>
 
@@ -138,19 +138,46 @@ size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t /
   return tl::attend_workspace(ctx, n_q_heads, n_rows);
 }
 
-int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
-              const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
-              float* d_lse, void* d_workspace, size_t workspace_bytes) {
-  if (!ctx) return TL_EINVAL;
+// What tl_attend and tl_attend_tree check alike (`fine`: what each has besides); *go:
+// whether there is something to do.
+static int check_attend(const tl_ctx* ctx, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads, const tl_rows* q,
+                        const tl_cache* cache, float scale, const tl_rows* out, const float* d_lse, const void* d_workspace,
+                        size_t workspace_bytes, bool fine, bool* go) {
+  *go = false;
   int r = check_layer(ctx, layer, cache);
   if (r) return r;
   if ((r = check_batch(batch))) return r;
-  if (!heads_ok(ctx, n_q_heads) || (flags & ~uint32_t(TL_ATTEND_ALL)) || !isfinite(scale)) return TL_EINVAL;
+  if (!heads_ok(ctx, n_q_heads) || !fine || !isfinite(scale)) return TL_EINVAL;
   if (batch->n_rows == 0 || batch->n_reqs == 0) return TL_OK;
   if (!rows_ok(q) || !result_ok(out, batch->n_rows, n_q_heads, ctx->D)) return TL_EINVAL;
   if (!d_workspace || ((uintptr_t)d_workspace & 15) || ((uintptr_t)d_lse & 3)) return TL_EINVAL;
   if (workspace_bytes < tl::attend_needs(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
+  *go = true;
+  return TL_OK;
+}
+
+int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
+              const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
+              float* d_lse, void* d_workspace, size_t workspace_bytes) {
+  if (!ctx) return TL_EINVAL;
+  bool go;
+  const int r = check_attend(ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_workspace, workspace_bytes,
+                             !(flags & ~uint32_t(TL_ATTEND_ALL)), &go);
+  if (!go) return r;
   return tl::launch_attend(ctx, stream, layer, batch, n_q_heads, q, cache, scale, flags, out, d_lse, d_workspace);
+}
+
+int tl_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_tree* tree,
+                   uint32_t n_q_heads, const tl_rows* q, const tl_cache* cache, float scale, const tl_rows* out,
+                   float* d_lse, void* d_workspace, size_t workspace_bytes) {
+  if (!ctx) return TL_EINVAL;
+  bool go;
+  const int r = check_attend(ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_workspace, workspace_bytes,
+                             tree && tree->words && tree->words <= 1u << 18, &go);
+  if (!go) return r;
+  if (!tree->d_seen || ((uintptr_t)tree->d_seen & 7) || !maybe_words(tree->d_pos)) return TL_EINVAL;
+  if (ctx->window[layer] && !tree->d_pos) return TL_EINVAL;
+  return tl::launch_attend_tree(ctx, stream, layer, batch, tree, n_q_heads, q, cache, scale, out, d_lse, d_workspace);
 }
 
 int tl_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, size_t n, const int32_t* d_src,

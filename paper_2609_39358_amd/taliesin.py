@@ -86,23 +86,28 @@ class tl_norm(ctypes.Structure):
                 ("k_stride", ctypes.c_int64), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
+class tl_tree(ctypes.Structure):
+    _fields_ = [("d_seen", ctypes.c_void_p), ("d_pos", ctypes.c_void_p), ("words", ctypes.c_uint32)]
+
+
 class tl_pool(ctypes.Structure):
     _fields_ = [("d_refs", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
 
 
 # torch's types of the operators' arguments, where torch is there
 _BF16 = None
-_WORDS = _FLOATS = _BYTES = ()
+_WORDS = _LONGS = _FLOATS = _BYTES = ()
 
 
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError("libtaliesin.so is not built (python -m paper_2609_39358_amd.build)")
-    global _BF16, _WORDS, _FLOATS, _BYTES
+    global _BF16, _WORDS, _LONGS, _FLOATS, _BYTES
     try:  # bind the library's HIP calls to the runtime torch has already loaded
         import torch
         _BF16 = torch.bfloat16
         _WORDS, _FLOATS = (torch.int32, torch.uint32, torch.uint8), (torch.float32,)
+        _LONGS = (torch.int64, torch.uint64)
         _BYTES = (torch.uint8, torch.int8, torch.bool)
     except ImportError:
         pass
@@ -153,6 +158,8 @@ def _load():
         "tl_attend_workspace_bytes": (c.c_size_t, [P, c.c_uint32, c.c_size_t, c.c_size_t]),
         "tl_attend": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.c_uint32, c.POINTER(tl_rows),
                                 c.POINTER(tl_cache), c.c_float, c.c_uint32, c.POINTER(tl_rows), P, P, c.c_size_t]),
+        "tl_attend_tree": (c.c_int, [P, P, c.c_uint32, c.POINTER(tl_batch), c.POINTER(tl_tree), c.c_uint32, c.POINTER(tl_rows),
+                                     c.POINTER(tl_cache), c.c_float, c.POINTER(tl_rows), P, P, c.c_size_t]),
         "tl_pages_copy": (c.c_int, [P, P, c.POINTER(tl_cache), c.c_size_t, P, P, P]),
         "tl_pages_fork": (c.c_int, [P, P, c.POINTER(tl_pool), c.POINTER(tl_cache), c.c_size_t, P, P, c.c_size_t, P, P, P,
                                     c.c_size_t, P, P, c.c_size_t]),
@@ -189,7 +196,7 @@ EXPORTED = (
     "tl_dindex_bytes", "tl_dindex_create", "tl_dindex_destroy", "tl_dindex_workspace_bytes",
     "tl_dindex_put", "tl_dindex_get", "tl_dindex_stats", "tl_chain_lookup", "tl_chain_stage",
     "tl_block_fingerprints", "tl_chain_lookup_par", "tl_append", "tl_append_norm", "tl_attend_workspace_bytes",
-    "tl_attend",
+    "tl_attend", "tl_attend_tree",
     "tl_pages_copy", "tl_pages_fork", "tl_pages_take", "tl_pages_free", "tl_pages_workspace_bytes", "tl_keep",
     "tl_file_open", "tl_file_close", "tl_file_records",
     "tl_file_read", "tl_file_write", "tl_file_drop_cache",
@@ -723,10 +730,24 @@ def tl_attend_workspace_bytes(ctx: Ctx, n_q_heads: int, n_reqs: int, n_rows: int
     return int(_lib.tl_attend_workspace_bytes(ctx.handle, n_q_heads, n_reqs, n_rows))
 
 
+def make_tree(d_seen, d_pos=None) -> tl_tree:
+    """Drafted tokens (tl_tree): d_seen i64 [n_rows, words], bit i of a row's words: it sees its
+    request's new token i; d_pos i32 [n_rows], their positions, for layers with a window."""
+    _of_type(d_seen, _LONGS, "masks")
+    _of_type(d_pos, _WORDS, "positions")
+    if d_seen.dim() != 2 or d_seen.element_size() != 8:
+        raise ValueError("masks have shape %s" % (tuple(d_seen.shape),))
+    _fits(d_seen, 0, "masks")
+    t = tl_tree(_addr(d_seen), _addr(d_pos), d_seen.shape[1])
+    t._keep = (d_seen, d_pos)
+    return t
+
+
 def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q, out, d_workspace, workspace_bytes: int,
-              scale: Optional[float] = None, lse=None, all_keys: bool = False):
+              scale: Optional[float] = None, lse=None, all_keys: bool = False, tree: Optional[tl_tree] = None):
     """Attention of q [n_rows, n_q_heads, head_dim] over the cache into out;
-    scale: head_dim ** -0.5 by default; all_keys: TL_ATTEND_ALL."""
+    scale: head_dim ** -0.5 by default; all_keys: TL_ATTEND_ALL; tree: the new
+    rows see each other as its masks say (tl_attend_tree)."""
     _check_operator(ctx, batch, cache)
     n, dim, shape = batch.n_rows, ctx.head_dim, q.shape
     if shape != out.shape:
@@ -734,11 +755,21 @@ def tl_attend(ctx: Ctx, stream, layer: int, batch: tl_batch, cache: tl_cache, q,
     _of_type(lse, _FLOATS, "lse")
     _fits(lse, 4 * n * shape[1], "lse")
     _fits(d_workspace, workspace_bytes, "workspace")
-    st = _lib.tl_attend(ctx.handle, _stream(stream), layer, batch, shape[1], _rows(q, n, dim, "queries"), cache,
-                        dim ** -0.5 if scale is None else scale, TL_ATTEND_ALL if all_keys else 0,
-                        _rows(out, n, dim, "results"), _addr(lse), _addr(d_workspace), workspace_bytes)
+    q, out, scale = _rows(q, n, dim, "queries"), _rows(out, n, dim, "results"), dim ** -0.5 if scale is None else scale
+    if tree is None:
+        st = _lib.tl_attend(ctx.handle, _stream(stream), layer, batch, shape[1], q, cache, scale, TL_ATTEND_ALL if all_keys else 0,
+                            out, _addr(lse), _addr(d_workspace), workspace_bytes)
+    else:
+        if all_keys:
+            raise ValueError("a tree's rows do not see all keys")
+        keep = getattr(tree, "_keep", None)
+        if keep is not None:
+            _fits(keep[0], 8 * n * tree.words, "masks")
+            _fits(keep[1], 4 * n, "positions")
+        st = _lib.tl_attend_tree(ctx.handle, _stream(stream), layer, batch, tree, shape[1], q, cache, scale, out, _addr(lse),
+                                 _addr(d_workspace), workspace_bytes)
     if st:
-        _check(st, "tl_attend")
+        _check(st, "tl_attend" if tree is None else "tl_attend_tree")
 
 
 # ------------------------------------------------------------------ pages of a cache
