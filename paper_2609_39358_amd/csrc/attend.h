@@ -63,12 +63,15 @@ struct AttendArgs {
   Share* share;              // [workers]
   float* part_ml;            // [2 * workers][slot_rows][2]
   float* part_o;             // [2 * workers][slot_rows][D]
-  const uint64_t* tree;      // [rows][tree_words] which of its request's new tokens a row sees, with TREE
+  const uint64_t* tree;      // [rows][tree_words] which of its request's new tokens a row sees, of a tree
   const int32_t* tree_pos;   // [rows] positions, where there is a window
   uint32_t tree_words;
 };
 
 namespace {
+
+// What the code is for: a text's rows, or a tree's.
+enum { kText, kTree };
 
 constexpr int kPlan = 256;  // threads that make a plan
 constexpr float kNone = -__builtin_inff();
@@ -114,12 +117,12 @@ struct Span {
   uint32_t b0, n;  // blocks of keys from b0 on; at least one, so that every tile has a worker
 };
 
-template <bool TREE>
+template <int MODE>
 __device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, uint32_t tile) {
   Span s;
   s.lo = 0;
   s.hi = q.held;
-  if constexpr (TREE) {  // any row may see any new token, and stands behind the ones before them
+  if constexpr (MODE != kText) {  // any row may see any new token, and stands behind the ones before them
     if (a.window) s.lo = (int)max((int64_t)0, (int64_t)q.before + 1 - (int64_t)a.window);
   } else if (!a.all) {
     const int t0 = (int)(tile * q.tile_rows), t1 = (int)min(tile * q.tile_rows + q.tile_rows, q.rows);
@@ -134,10 +137,10 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, u
 }
 
 // Units of a request's tiles tile0, tile0 + step, ...
-template <bool TREE>
+template <int MODE>
 __device__ __forceinline__ uint64_t units_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
   uint64_t n = 0;
-  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + q.weight * span_of<TREE>(a, q, t).n;
+  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + q.weight * span_of<MODE>(a, q, t).n;
   return n;
 }
 
@@ -161,7 +164,7 @@ struct PlanLds {
   uint32_t found;
 };
 
-template <bool TREE>
+template <int MODE>
 __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   const uint32_t tid = threadIdx.x, n = a.b.n_reqs;
   // threads for each request (few requests), or requests for each thread
@@ -172,12 +175,12 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   if (split > 1) {
     if (tid / split < n) {
       const Request q = request_of(a, tid / split);
-      mine = units_of<TREE>(a, q, tid % split, split) * q.heads;
+      mine = units_of<MODE>(a, q, tid % split, split) * q.heads;
     }
   } else if (tid < kPlan) {
     for (uint32_t r = tid * per; r < min(tid * per + per, n); ++r) {
       const Request q = request_of(a, r);
-      mine += units_of<TREE>(a, q, 0, 1) * q.heads;
+      mine += units_of<MODE>(a, q, 0, 1) * q.heads;
     }
   }
   uint64_t incl = mine;
@@ -216,13 +219,13 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
   c.first = uniform(l.found_at);
   while (c.r < n) {
     const Request q = uniform(request_of(a, c.r));
-    const uint64_t units = split > 1 ? uniform(l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : units_of<TREE>(a, q, 0, 1);
+    const uint64_t units = split > 1 ? uniform(l.sum[(c.r + 1) * split] - l.sum[c.r * split]) / q.heads : units_of<MODE>(a, q, 0, 1);
     if (c.at < c.first + units * q.heads) {
       c.head = (uint32_t)((c.at - c.first) / units);
       c.first += c.head * units;
       c.tile = 0;
       for (;;) {
-        const uint32_t k = q.cost + q.weight * span_of<TREE>(a, q, c.tile).n;
+        const uint32_t k = q.cost + q.weight * span_of<MODE>(a, q, c.tile).n;
         if (c.at < c.first + k) return true;
         c.first += k;
         ++c.tile;
@@ -278,7 +281,7 @@ struct Place {
   int lo, hi;  // it sees keys [lo, hi); of a tree those before the new tokens, and of those what its mask names
 };
 
-template <bool TREE>
+template <int MODE>
 __device__ __forceinline__ Place place_of(const AttendArgs& a, const Kind& k, const Request& q, uint32_t head, uint32_t tile, uint32_t m) {
   Place p;
   const uint32_t part = head % k.parts, kv = head / k.parts;
@@ -289,7 +292,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, const Kind& k, co
   p.head = kv * a.group + (p.there ? g : 0);
   p.lo = 0;
   p.hi = q.held;
-  if constexpr (TREE) {
+  if constexpr (MODE != kText) {
     if (a.window) {
       const int position = min(max(a.tree_pos[p.row], q.before), q.before + (int)q.rows - 1);
       p.lo = (int)max((int64_t)0, min((int64_t)q.before, (int64_t)position + 1 - (int64_t)a.window));
@@ -520,7 +523,7 @@ struct Rows16 {
   Soft s;
 };
 
-template <int D, bool FP8, bool EVEN, bool TREE>
+template <int D, bool FP8, bool EVEN, int MODE>
 __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, uint32_t kv, int key0, const Place& p, int before, bool edge,
                                         bool several, uint32_t& odd, Rows16<D, FP8>& r) {
   typedef Tile16<D, FP8> Tile;
@@ -560,12 +563,12 @@ __device__ __forceinline__ void block16(const AttendArgs& a, Tile16<D, FP8>& t, 
     for (int i = 0; i < 4; ++i) x[4 * h + i] = acc[i];
   }
   if (edge || t.seen != ~0ull) {  // some row does not see some key
-    const uint64_t sees = TREE ? named(a, p.row, key0 - before) : ~0ull;
+    const uint64_t sees = MODE != kText ? named(a, p.row, key0 - before) : ~0ull;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int at = (i / 4) * 16 + quad * 4 + i % 4;
       const bool there = t.seen >> at & 1;
-      x[i] = there && key0 + at >= p.lo && key0 + at < p.hi && (!TREE || (sees >> at & 1)) ? x[i] : kNone;
+      x[i] = there && key0 + at >= p.lo && key0 + at < p.hi && (MODE == kText || (sees >> at & 1)) ? x[i] : kNone;
       if (!there) {  // whatever a page holds there, it may be NaN
 #pragma unroll
         for (int j = 0; j < Tile::kVWords; ++j) t.v[i][j] = 0;
@@ -636,7 +639,7 @@ struct Lds16 {
 
 // The cursor's blocks of one tile of 16 rows for each of a workgroup's runs of
 // heads, up to the cursor's end or the tile's.
-template <int D, bool FP8, bool EVEN, int WAVES, bool TREE>
+template <int D, bool FP8, bool EVEN, int WAVES, int MODE>
 __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& l, const Cursor& cur, const Request& q, const Span& s,
                                           uint32_t k0, uint32_t k1) {
   constexpr int M = 16, E = D / 16;
@@ -649,7 +652,7 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   const int32_t* table = a.b.table + (uint64_t)cur.r * a.b.width;
   const uint32_t head = (cur.head << hs) + (wave & (heads - 1)), sub = wave >> hs;
   const uint32_t kv = head / kind.parts;
-  const Place p = place_of<TREE>(a, kind, q, head, cur.tile, c);
+  const Place p = place_of<MODE>(a, kind, q, head, cur.tile, c);
   Rows16<D, FP8> r;
   r.s = Soft{kNone, 0.f, 0.f};
 #pragma unroll
@@ -662,11 +665,11 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   }
   // keys below first_hi and from last_lo on are seen by all rows of the tile
   const int t0 = (int)(cur.tile * kind.tile_rows), t1 = (int)min(cur.tile * kind.tile_rows + kind.tile_rows, q.rows);
-  const int first_hi = TREE ? min(q.held, q.before) : a.all ? q.held : min(q.held, q.before + t0 + 1);
-  const int last_lo = a.window ? (int)max((int64_t)0, (int64_t)q.before + (TREE ? (int)q.rows : t1) - (int64_t)a.window) : 0;
+  const int first_hi = MODE != kText ? min(q.held, q.before) : a.all ? q.held : min(q.held, q.before + t0 + 1);
+  const int last_lo = a.window ? (int)max((int64_t)0, (int64_t)q.before + (MODE != kText ? (int)q.rows : t1) - (int64_t)a.window) : 0;
 
   const int key0 = (int)(s.b0 + k0) * step + (int)sub * Tile::kKeys, last = (int)(s.b0 + k1 - 1) * step + (int)sub * Tile::kKeys;
-  const bool several = TREE || (!a.all && t1 - t0 > 1);  // rows that see different keys, or not all that lie between them
+  const bool several = MODE != kText || (!a.all && t1 - t0 > 1);  // rows that see different keys, or not all that lie between them
   auto edge = [&](int key) { return key + Tile::kKeys > first_hi || key < last_lo; };
   uint32_t odd = 0;
   if (s.hi > s.lo) {
@@ -688,11 +691,11 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     int key = key0;
     for (; key + step <= last; key += 2 * step) {  // no way out in between: it would have every load waited for
       next(key + step, tb);
-      block16<D, FP8, EVEN, TREE>(a, ta, kv, key, p, q.before, edge(key), several, odd, r);
+      block16<D, FP8, EVEN, MODE>(a, ta, kv, key, p, q.before, edge(key), several, odd, r);
       next(key + 2 * step, ta);
-      block16<D, FP8, EVEN, TREE>(a, tb, kv, key + step, p, q.before, edge(key + step), several, odd, r);
+      block16<D, FP8, EVEN, MODE>(a, tb, kv, key + step, p, q.before, edge(key + step), several, odd, r);
     }
-    if (key <= last) block16<D, FP8, EVEN, TREE>(a, ta, kv, key, p, q.before, edge(key), several, odd, r);
+    if (key <= last) block16<D, FP8, EVEN, MODE>(a, ta, kv, key, p, q.before, edge(key), several, odd, r);
   }
 
   if (several && __any(odd)) {
@@ -700,7 +703,7 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
     for (int key = key0; key <= last; key += step) {
       if (!edge(key)) continue;
       odd_keys<D, FP8>(a, table, vp, kv, max(key, s.lo), min(key + Tile::kKeys, s.hi), [&](int at, GlobalBytes v) {
-        if (at < p.lo || at >= p.hi || (TREE && !(named(a, p.row, at - q.before) & 1))) return;
+        if (at < p.lo || at >= p.hi || (MODE != kText && !(named(a, p.row, at - q.before) & 1))) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -762,7 +765,7 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
   // each thread: E elements of a row
   for (uint32_t f = tid / 16; f < heads * M; f += 4 * WAVES) {
     const uint32_t h = f / M, m = f % M, d0 = tid % 16 * E;
-    const Place pm = place_of<TREE>(a, kind, q, (cur.head << hs) + h, cur.tile, m);
+    const Place pm = place_of<MODE>(a, kind, q, (cur.head << hs) + h, cur.tile, m);
     if (!pm.there) continue;
     float row_top = kNone, row_sum = 0.f, y[E];
     for (uint32_t w = h; w < WAVES; w += heads) row_top = fmaxf(row_top, l.m[w][m]);
@@ -779,25 +782,25 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
 // Tiles of 16 rows for all requests. One token over 97,000 in scaled pages of 16
 // heads of 128: 78 us, 5.1 TB/s (a large copy reaches 4.7); 64 requests of up to
 // 32,768 164 us, 5.2 TB/s.
-template <int D, bool FP8, bool EVEN, bool TREE>
+template <int D, bool FP8, bool EVEN, int MODE>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a) {
   __shared__ union {
     PlanLds plan;
     Lds16<D, 4> s;
   } l;
   Cursor cur;
-  const bool any = plan<TREE>(a, l.plan, cur);
+  const bool any = plan<MODE>(a, l.plan, cur);
   if (!any) {
     if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
   Request q = uniform(request_of(a, cur.r));
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Span s = span_of<TREE>(a, q, cur.tile);
+    const Span s = span_of<MODE>(a, q, cur.tile);
     uint32_t k0, k1;
     const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
-    if (k0 < k1) segment16<D, FP8, EVEN, 4, TREE>(a, l.s, cur, q, s, k0, k1);
+    if (k0 < k1) segment16<D, FP8, EVEN, 4, MODE>(a, l.s, cur, q, s, k0, k1);
     cur.at = min(cur.end, tile_end);
     if (cur.at == tile_end) {
       cur.first = tile_end;
@@ -866,7 +869,7 @@ __device__ __forceinline__ uint32_t v_at(uint32_t r, uint32_t elem) {
   return r * D + (elem ^ v_swap<D>(r));
 }
 
-template <int D, bool FP8, int WAVES, bool TREE>
+template <int D, bool FP8, int WAVES, int MODE>
 __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l, const Cursor& cur, const Request& q, const Span& s,
                                           uint32_t k0, uint32_t k1) {
   constexpr int R = rows_of_wave(D), KT = LdsMany<D>::KT, kThreads = 64 * WAVES;
@@ -893,7 +896,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   int row_lo, row_hi;  // keys that this lane's row sees
   uint32_t row_at;     // its row of the batch
   {
-    const Place p = place_of<TREE>(a, kind, q, cur.head, cur.tile, m);
+    const Place p = place_of<MODE>(a, kind, q, cur.head, cur.tile, m);
     const uint16_t* qp = a.q + (int64_t)p.row * a.q_token + (int64_t)p.head * a.q_head;
 #pragma unroll
     for (int k = 0; k < D / kDepth; ++k) qf[k] = load_q(a, qp + k * kDepth + part * 8, p.there);
@@ -907,14 +910,14 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   {
     const uint32_t tokens = min(kind.tile_rows, q.rows - cur.tile * kind.tile_rows);
     const uint32_t t0 = wave * R / kind.part_heads, t1 = min((wave * R + R - 1) / kind.part_heads, tokens - 1);
-    if (TREE && t0 < tokens) {
+    if (MODE != kText && t0 < tokens) {
       wave_lo = s.lo;
       wave_hi = q.held;
       all_hi = min(q.held, q.before);
       if (a.window) all_lo = (int)max((int64_t)0, (int64_t)q.before + q.rows - (int64_t)a.window);
     } else if (t0 < tokens) {
-      const Place p0 = place_of<TREE>(a, kind, q, cur.head, cur.tile, t0 * kind.part_heads);
-      const Place p1 = place_of<TREE>(a, kind, q, cur.head, cur.tile, t1 * kind.part_heads);
+      const Place p0 = place_of<MODE>(a, kind, q, cur.head, cur.tile, t0 * kind.part_heads);
+      const Place p1 = place_of<MODE>(a, kind, q, cur.head, cur.tile, t1 * kind.part_heads);
       wave_lo = uniform(p0.lo);
       wave_hi = uniform(p1.hi);
       all_lo = uniform(p1.lo);
@@ -998,7 +1001,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   // others (whose weight is 0, but 0 times infinity is NaN), and no page is missing:
   // their values are kept as they are.
   int all_from = s.lo, all_to = s.hi;
-  if constexpr (TREE) {
+  if constexpr (MODE != kText) {
     all_to = min(all_to, q.before);
     if (a.window) all_from = max(all_from, (int)max((int64_t)0, (int64_t)q.before + q.rows - (int64_t)a.window));
   } else if (!a.all) {
@@ -1100,13 +1103,13 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
           const bool in = key >= row_lo && key < row_hi;
           if (!in || (uint32_t)table[a.b.page.div((uint32_t)key)] >= a.c.n_pages) bits &= ~(1u << t);
         }
-      const uint64_t sees = TREE ? named(a, row_at, first - q.before) : ~0ull;
+      const uint64_t sees = MODE != kText ? named(a, row_at, first - q.before) : ~0ull;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < S; ++j) {
           const int key = first + R * b + 8 * (j / 4) + j % 4;
-          const bool there = (bits >> (S * b + j) & 1) && key >= row_lo && key < row_hi && (!TREE || (sees >> (key - first) & 1));
+          const bool there = (bits >> (S * b + j) & 1) && key >= row_lo && key < row_hi && (MODE == kText || (sees >> (key - first) & 1));
           x[b][j] = there ? x[b][j] : kNone;
         }
     }
@@ -1246,7 +1249,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
       if (n >= plain_lo && n < plain_hi) continue;
       const int key0 = block0 + n * KT;
       odd_keys<D, FP8>(a, table, vp, kv, max(key0, s.lo), min(key0 + KT, s.hi), [&](int key, GlobalBytes v) {
-        if (key < row_lo || key >= row_hi || (TREE && !(named(a, row_at, key - q.before) & 1))) return;
+        if (key < row_lo || key >= row_hi || (MODE != kText && !(named(a, row_at, key - q.before) & 1))) return;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -1262,7 +1265,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
   if constexpr (R == 16) sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   const bool whole = k0 == 0 && k1 == s.n;
-  const Place p = place_of<TREE>(a, kind, q, cur.head, cur.tile, m);
+  const Place p = place_of<MODE>(a, kind, q, cur.head, cur.tile, m);
   if (p.there) {
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const uint64_t slot = (2 * (uint64_t)cur.worker + (k0 > 0 ? 0 : 1)) * a.slot_rows;
@@ -1298,7 +1301,7 @@ __device__ __forceinline__ void segment_many(const AttendArgs& a, LdsMany<D>& l,
 //
 // Tiles of many rows, and of 16 for requests of few (heads of 256: their 16-row
 // tiles want the registers of one wavefront on a SIMD, and stay in k_attend16).
-template <int D, bool FP8, bool EVEN, int WAVES, bool TREE>
+template <int D, bool FP8, bool EVEN, int WAVES, int MODE>
 __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
   __shared__ union {
     PlanLds plan;
@@ -1306,23 +1309,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
     LdsMany<D> many;
   } l;
   Cursor cur;
-  const bool any = plan<TREE>(a, l.plan, cur);
+  const bool any = plan<MODE>(a, l.plan, cur);
   if (!any) {
     if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
   Request q = uniform(request_of(a, cur.r));
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Span s = span_of<TREE>(a, q, cur.tile);
+    const Span s = span_of<MODE>(a, q, cur.tile);
     uint32_t k0, k1;
     const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
     if (k0 == k1) {
       // none
     } else if (D == 256 || q.kind) {
-      segment_many<D, FP8, WAVES, TREE>(a, l.many, cur, q, s, k0, k1);
+      segment_many<D, FP8, WAVES, MODE>(a, l.many, cur, q, s, k0, k1);
     } else if constexpr (D != 256) {
-      segment16<D, FP8, EVEN, WAVES, TREE>(a, l.few, cur, q, s, k0, k1);
+      segment16<D, FP8, EVEN, WAVES, MODE>(a, l.few, cur, q, s, k0, k1);
     }
     cur.at = min(cur.end, tile_end);
     if (cur.at == tile_end) {
@@ -1361,7 +1364,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   for (uint32_t f = f0; f < end; f += kRuns) {
     const bool there = f + i < end;
     const uint32_t at_head = min(f + i, end - 1) / rows, m = min(f + i, end - 1) % rows, row = at_head * kind.rows + m;
-    const Place p = place_of<false>(a, kind, q, (sh.head << kind.heads_shift) + at_head, sh.tile, m);
+    const Place p = place_of<kText>(a, kind, q, (sh.head << kind.heads_shift) + at_head, sh.tile, m);
     float top = kNone, sum = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
     for (uint32_t w0 = slice; there && w0 < sh.parts; w0 += slices * kAhead) {
@@ -1446,6 +1449,27 @@ uint32_t waves_of(const tl_ctx* ctx, uint64_t per) {
   return per <= many ? 0 : per > eight ? 8 : 4;
 }
 
+// Sets how many workgroups join a tile of few rows; returns the rows of one, of all the
+// heads that a workgroup takes.
+//
+// Tiles of many rows have few parts: a run of threads for each row. Tiles of few
+// rows may have many, if there are few tiles: so many runs for a row that each
+// has about 8 parts, which are on their way together. Four tiles of 8 rows of 128
+// parts: 8.2 us, with 2 of a workgroup's 8 runs for each row 12.1.
+uint64_t join_rows(Shape& s, const Kind& f, const tl_ctx* ctx, uint64_t n_reqs, uint64_t n_rows) {
+  const uint32_t runs_of_block = 1024 / ctx->D;
+  const uint64_t reqs = n_reqs ? n_reqs : 1, tokens = (n_rows + reqs - 1) / reqs;
+  const uint64_t rows = (tokens < f.tile_rows ? tokens : f.tile_rows) * f.part_heads << f.heads_shift;
+  if (!s.waves) {
+    uint64_t slices = s.workers / (reqs * f.heads) / 8;
+    slices = slices < 1 ? 1 : slices > runs_of_block ? runs_of_block : slices;
+    const uint64_t wanted = (rows * slices + runs_of_block - 1) / runs_of_block;
+    if (wanted < s.joins) s.joins = (uint32_t)wanted;
+    if (!s.joins) s.joins = 1;
+  }
+  return rows;
+}
+
 Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows, uint32_t waves) {
   Shape s;
   const uint32_t group = n_q_heads / ctx->H, wide = ctx->dtype == TL_DTYPE_FP8_SCALED ? 1 : 2;
@@ -1480,21 +1504,8 @@ Shape shape_of(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t 
   m.cost = 4 * m.weight;
   s.slot_rows = 16u << f.heads_shift;
   if (s.waves && s.slot_rows < m.rows) s.slot_rows = m.rows;
-  // Tiles of many rows have few parts: a run of threads for each row. Tiles of few
-  // rows may have many, if there are few tiles: so many runs for a row that each
-  // has about 8 parts, which are on their way together. Four tiles of 8 rows of 128
-  // parts: 8.2 us, with 2 of a workgroup's 8 runs for each row 12.1.
-  const uint32_t runs_of_block = 1024 / ctx->D;
-  const uint64_t reqs = n_reqs ? n_reqs : 1, tokens = (n_rows + reqs - 1) / reqs;
-  const uint64_t rows = (tokens < f.tile_rows ? tokens : f.tile_rows) * f.part_heads << f.heads_shift;
-  s.joins = s.slot_rows / runs_of_block;
-  if (!s.waves) {
-    uint64_t slices = s.workers / (reqs * f.heads) / 8;
-    slices = slices < 1 ? 1 : slices > runs_of_block ? runs_of_block : slices;
-    const uint64_t wanted = (rows * slices + runs_of_block - 1) / runs_of_block;
-    if (wanted < s.joins) s.joins = (uint32_t)wanted;
-    if (!s.joins) s.joins = 1;
-  }
+  s.joins = s.slot_rows / (1024 / ctx->D);
+  const uint64_t rows = join_rows(s, f, ctx, n_reqs, n_rows);
   // A part costs the join more the more rows it has, so a worker of a small batch
   // has to have some blocks. us with 1 / 2 / 3, 8 rows: 13 / 13 / 14 (1,024 keys),
   // 13 / 13 / 14 (4,096); 32 rows: 13 / 13 / 13, 25 / 21 / 18; 64 rows: 18 / 16 / 15, 36 / 25 / 21.
@@ -1518,34 +1529,41 @@ Layout layout_of(const Shape& s, uint32_t D) {
   return l;
 }
 
-template <int D, bool FP8, bool EVEN, bool TREE>
-void launch(const Shape& sh, hipStream_t s, const AttendArgs& a) {
-  {
-    TimedLaunch timed(TL_KERNEL_ATTEND, s);
-    const dim3 grid(sh.workers);
-    if (!sh.waves)
-      hipLaunchKernelGGL((k_attend16<D, FP8, EVEN, TREE>), grid, dim3(256), 0, s, a);
-    else if (sh.waves == 8)
-      hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 8, TREE>), grid, dim3(512), 0, s, a);
-    else if constexpr (D != 256)
-      hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 4, TREE>), grid, dim3(256), 0, s, a);
-  }
+template <int D>
+void launch_join(const Shape& sh, hipStream_t s, const AttendArgs& a) {
   TimedLaunch timed(TL_KERNEL_ATTEND_JOIN, s);
   hipLaunchKernelGGL((k_attend_join<D>), dim3((sh.workers - 1) * sh.joins), dim3(256), 0, s, a);
 }
 
-template <int D, bool TREE>
-void launch(bool fp8, bool even, const Shape& sh, hipStream_t s, const AttendArgs& a) {
-  if (fp8)
-    even ? launch<D, true, true, TREE>(sh, s, a) : launch<D, true, false, TREE>(sh, s, a);
-  else
-    even ? launch<D, false, true, TREE>(sh, s, a) : launch<D, false, false, TREE>(sh, s, a);
+template <int D, bool FP8, bool EVEN, int MODE>
+void launch_many(const Shape& sh, hipStream_t s, const AttendArgs& a) {
+  if (sh.waves == 8)
+    hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 8, MODE>), dim3(sh.workers), dim3(512), 0, s, a);
+  else if constexpr (D != 256)
+    hipLaunchKernelGGL((k_attend_many<D, FP8, EVEN, 4, MODE>), dim3(sh.workers), dim3(256), 0, s, a);
 }
 
-// Fills what both calls have in common, and launches.
-template <bool TREE>
-int launch(AttendArgs& a, const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads, const tl_rows* q,
-           const tl_cache* cache, float scale, const tl_rows* out, float* d_lse, void* d_ws) {
+// launch(D, FP8, EVEN) as types, for a context.
+template <class Launch>
+void by_cache(const tl_ctx* ctx, Launch launch) {
+  const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED, even = ctx->P % 16 == 0;
+  auto dim = [&](auto D) {
+    if (fp8)
+      even ? launch(D, std::true_type(), std::true_type()) : launch(D, std::true_type(), std::false_type());
+    else
+      even ? launch(D, std::false_type(), std::true_type()) : launch(D, std::false_type(), std::false_type());
+  };
+  if (ctx->D == 64)
+    dim(std::integral_constant<int, 64>());
+  else if (ctx->D == 128)
+    dim(std::integral_constant<int, 128>());
+  else
+    dim(std::integral_constant<int, 256>());
+}
+
+// What all calls have in common; the workspace's parts by the shape.
+void fill(AttendArgs& a, const Shape& sh, const tl_ctx* ctx, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads, const tl_rows* q,
+          const tl_cache* cache, float scale, const tl_rows* out, float* d_lse, void* d_ws) {
   fill_batch(a.b, ctx, layer, batch);
   fill_pages(a.c, ctx, layer, cache);
   a.q = (const uint16_t*)q->d_rows;
@@ -1557,7 +1575,6 @@ int launch(AttendArgs& a, const tl_ctx* ctx, void* stream, uint32_t layer, const
   a.lse = d_lse;
   a.n_heads = ctx->H;
   a.group = n_q_heads / ctx->H;
-  const Shape sh = shape_of(ctx, n_q_heads, batch->n_reqs, batch->n_rows);
   a.kind[0] = sh.kind[0];
   a.kind[1] = sh.kind[1];
   a.few = sh.few;
@@ -1572,15 +1589,6 @@ int launch(AttendArgs& a, const tl_ctx* ctx, void* stream, uint32_t layer, const
   a.share = (Share*)d_ws;
   a.part_ml = (float*)((uint8_t*)d_ws + lay.ml);
   a.part_o = (float*)((uint8_t*)d_ws + lay.o);
-  hipStream_t s = (hipStream_t)stream;
-  (void)hipGetLastError();
-  const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED, even = ctx->P % 16 == 0;
-  switch (ctx->D) {
-    case 64: launch<64, TREE>(fp8, even, sh, s, a); break;
-    case 128: launch<128, TREE>(fp8, even, sh, s, a); break;
-    default: launch<256, TREE>(fp8, even, sh, s, a); break;
-  }
-  return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE;
 }
 
 }  // namespace

@@ -21,7 +21,21 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
                   const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out, float* d_lse, void* d_ws) {
   AttendArgs a = {};
   a.all = (flags & TL_ATTEND_ALL) != 0;
-  return launch<false>(a, ctx, stream, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_ws);
+  const Shape sh = shape_of(ctx, n_q_heads, batch->n_reqs, batch->n_rows);
+  fill(a, sh, ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_ws);
+  hipStream_t s = (hipStream_t)stream;
+  (void)hipGetLastError();
+  by_cache(ctx, [&](auto D, auto fp8, auto even) {
+    {
+      TimedLaunch timed(TL_KERNEL_ATTEND, s);
+      if (sh.waves)
+        launch_many<D(), fp8(), even(), kText>(sh, s, a);
+      else
+        hipLaunchKernelGGL((k_attend16<D(), fp8(), even(), kText>), dim3(sh.workers), dim3(256), 0, s, a);
+    }
+    launch_join<D()>(sh, s, a);
+  });
+  return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE;
 }
 
 }  // namespace tl

@@ -120,6 +120,8 @@ size_t attend_workspace(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_rows);
 int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads,
                   const tl_rows* q, const tl_cache* cache, float scale, uint32_t flags, const tl_rows* out,
                   float* d_lse, void* d_ws);
+size_t attend_tree_needs(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows);
+size_t attend_tree_workspace(const tl_ctx* ctx, uint32_t n_q_heads);
 int launch_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* batch, const tl_tree* tree, uint32_t n_q_heads,
                        const tl_rows* q, const tl_cache* cache, float scale, const tl_rows* out, float* d_lse, void* d_ws);
 

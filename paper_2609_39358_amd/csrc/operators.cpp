@@ -3,6 +3,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "internal.h"
 
 namespace {
@@ -135,14 +137,14 @@ int tl_append_norm(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_bat
 
 size_t tl_attend_workspace_bytes(const tl_ctx* ctx, uint32_t n_q_heads, size_t /*n_reqs*/, size_t n_rows) {
   if (!ctx || !heads_ok(ctx, n_q_heads)) return 0;
-  return tl::attend_workspace(ctx, n_q_heads, n_rows);
+  return std::max(tl::attend_workspace(ctx, n_q_heads, n_rows), tl::attend_tree_workspace(ctx, n_q_heads));
 }
 
 // What tl_attend and tl_attend_tree check alike (`fine`: what each has besides); *go:
 // whether there is something to do.
 static int check_attend(const tl_ctx* ctx, uint32_t layer, const tl_batch* batch, uint32_t n_q_heads, const tl_rows* q,
                         const tl_cache* cache, float scale, const tl_rows* out, const float* d_lse, const void* d_workspace,
-                        size_t workspace_bytes, bool fine, bool* go) {
+                        size_t workspace_bytes, size_t (*needs)(const tl_ctx*, uint32_t, uint64_t, uint64_t), bool fine, bool* go) {
   *go = false;
   int r = check_layer(ctx, layer, cache);
   if (r) return r;
@@ -151,7 +153,7 @@ static int check_attend(const tl_ctx* ctx, uint32_t layer, const tl_batch* batch
   if (batch->n_rows == 0 || batch->n_reqs == 0) return TL_OK;
   if (!rows_ok(q) || !result_ok(out, batch->n_rows, n_q_heads, ctx->D)) return TL_EINVAL;
   if (!d_workspace || ((uintptr_t)d_workspace & 15) || ((uintptr_t)d_lse & 3)) return TL_EINVAL;
-  if (workspace_bytes < tl::attend_needs(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
+  if (workspace_bytes < needs(ctx, n_q_heads, batch->n_reqs, batch->n_rows)) return TL_ERANGE;
   *go = true;
   return TL_OK;
 }
@@ -162,7 +164,7 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
   if (!ctx) return TL_EINVAL;
   bool go;
   const int r = check_attend(ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_workspace, workspace_bytes,
-                             !(flags & ~uint32_t(TL_ATTEND_ALL)), &go);
+                             tl::attend_needs, !(flags & ~uint32_t(TL_ATTEND_ALL)), &go);
   if (!go) return r;
   return tl::launch_attend(ctx, stream, layer, batch, n_q_heads, q, cache, scale, flags, out, d_lse, d_workspace);
 }
@@ -173,7 +175,7 @@ int tl_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_bat
   if (!ctx) return TL_EINVAL;
   bool go;
   const int r = check_attend(ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_workspace, workspace_bytes,
-                             tree && tree->words && tree->words <= 1u << 18, &go);
+                             tl::attend_tree_needs, tree && tree->words && tree->words <= 1u << 18, &go);
   if (!go) return r;
   if (!tree->d_seen || ((uintptr_t)tree->d_seen & 7) || !maybe_words(tree->d_pos)) return TL_EINVAL;
   if (ctx->window[layer] && !tree->d_pos) return TL_EINVAL;
