@@ -32,26 +32,26 @@ constexpr uint32_t kPiece = kThreads * kFlight * 16;          // bytes that a wo
 constexpr uint32_t kMostGroups = 1u << 22;                    // workgroups of a launch; further work is looped over
 
 // ---- copying ---------------------------------------------------------------------
-// One workgroup's piece of a page's first `rows` rows, and of its scales with the
-// first piece. Bounded by memory: every byte is read and written once.
-__device__ __forceinline__ void copy_piece(const Slabs& c, uint32_t slab, uint32_t src, uint32_t dst, uint32_t rows, uint32_t piece) {
+// One workgroup's pieces of a page's first `rows` rows (every `pieces`th from `piece` on),
+// and the page's scales with the first. Bounded by memory: every byte is read and written
+// once, and not expected back soon.
+__device__ __forceinline__ void copy_pieces(const Slabs& c, uint32_t slab, uint32_t src, uint32_t dst, uint32_t rows, uint32_t piece, uint32_t pieces) {
   const Bytes base = (Bytes)c.base(slab);
   const Bytes from = base + (int64_t)src * c.stride, to = base + (int64_t)dst * c.stride;
   const uint32_t bytes = rows * c.row_bytes, whole = bytes & ~15u, tid = threadIdx.x;
-  const uint32_t at = piece * kPiece + tid * 16;
-  u32x4 x[kFlight];
+  for (uint32_t at = piece * kPiece + tid * 16; at < whole; at += pieces * kPiece) {
+    u32x4 x[kFlight];
 #pragma unroll
-  for (uint32_t i = 0; i < kFlight; ++i)
-    if (at + i * kThreads * 16 < whole) x[i] = *(Granules)(from + at + i * kThreads * 16);
+    for (uint32_t i = 0; i < kFlight; ++i)
+      if (at + i * kThreads * 16 < whole) x[i] = __builtin_nontemporal_load((Granules)(from + at + i * kThreads * 16));
 #pragma unroll
-  for (uint32_t i = 0; i < kFlight; ++i)
-    if (at + i * kThreads * 16 < whole) *(Granules)(to + at + i * kThreads * 16) = x[i];
+    for (uint32_t i = 0; i < kFlight; ++i)
+      if (at + i * kThreads * 16 < whole) __builtin_nontemporal_store(x[i], (Granules)(to + at + i * kThreads * 16));
+  }
   if (piece) return;
   if (whole + tid < bytes) to[whole + tid] = from[whole + tid];  // rows that end within sixteen bytes
   for (uint32_t i = tid; i < c.n_scales; i += kThreads) to[c.code_bytes + i] = from[c.code_bytes + i];
 }
-
-__host__ __device__ __forceinline__ uint32_t pieces_of(uint32_t bytes) { return bytes < kPiece ? 1 : (bytes + kPiece - 1) / kPiece; }
 
 struct CopyArgs {
   Slabs c;
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void k_pages_copy(CopyArgs a) {
     const uint32_t src = (uint32_t)a.src[at], dst = (uint32_t)a.dst[at];
     if (src >= a.c.n_pages || dst >= a.c.n_pages || src == dst) continue;
     const uint32_t rows = a.rows ? min(a.rows[i], a.c.page_tokens) : a.c.page_tokens;
-    copy_piece(a.c, slab, src, dst, rows, piece);
+    copy_pieces(a.c, slab, src, dst, rows, piece, a.pieces);
   }
 }
 
@@ -149,8 +149,11 @@ __device__ uint32_t wanted(const PoolArgs& a, uint32_t r, uint32_t g) {
     bool fine = true;
     if (r < a.n) range_of(a, r, c0, c1, fine);
     const int32_t* row = a.out_tables + ((uint64_t)g * a.n + min(r, a.n - 1)) * a.width;
-    if (c1 - c0 <= kShort)
-      for (uint32_t c = c0; c < c1; ++c) n += row[c] < 0;
+    if (c1 - c0 <= kShort) {
+#pragma unroll
+      for (uint32_t i = 0; i < kShort; ++i)
+        if (c0 + i < c1) n += row[c0 + i] < 0;
+    }
     for (uint64_t m = __ballot(c1 - c0 > kShort); m; m &= m - 1) {
       const uint32_t lane = (uint32_t)__builtin_ctzll(m), who = __shfl(r, lane), b0 = __shfl(c0, lane), b1 = __shfl(c1, lane);
       const int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + who) * a.width;
@@ -163,19 +166,34 @@ __device__ uint32_t wanted(const PoolArgs& a, uint32_t r, uint32_t g) {
   }
 }
 
-// One workgroup: what every request wants, the lowest free pages, who is served;
-// tl_pages_take's entries. Some microseconds that follow each other: a step of a
-// batch asks for it once, for all layers.
+// One workgroup: what every request wants, the lowest free pages, who is served, and
+// tl_pages_take's entries. A chain of loads that wait for each other (some 1 us each), so
+// the first pages' counts are asked for before the requests' wishes, and what a thread
+// knows of its request stays in registers where there is a thread for each.
 template <bool FORK>
 __global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
-  __shared__ uint32_t sums[kPlanWaves], cnt[kScan][kPlanWaves], found[TL_MAX_GROUPS];
+  __shared__ uint32_t sums[kPlanWaves], before_of[kScan * kPlanWaves], found_now, found[TL_MAX_GROUPS];
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
-  for (uint32_t g = 0; g < a.n_groups; ++g) {
+  const bool one = a.n <= kPlanThreads;  // a thread for each request
+  uint32_t at[TL_MAX_GROUPS], mine[TL_MAX_GROUPS];
+  int32_t held[kScan];
+  auto ask = [&](const int32_t* refs, uint64_t p0) {
+#pragma unroll
+    for (uint32_t k = 0; k < kScan; ++k) {
+      const uint64_t p = p0 + k * kPlanThreads + tid;
+      held[k] = p < a.n_pages ? refs[p] : 1;
+    }
+  };
+#pragma unroll
+  for (uint32_t g = 0; g < TL_MAX_GROUPS; ++g) {
+    if (g >= a.n_groups) break;
+    const int32_t* refs = a.refs + (uint64_t)g * a.n_pages;
+    ask(refs, 0);
     uint32_t* start = a.start + (uint64_t)g * (a.n + 1);
     uint32_t total = 0;
     for (uint32_t r0 = 0; r0 < a.n; r0 += kPlanThreads) {
-      const uint32_t r = r0 + tid, mine = wanted<FORK>(a, r, g);
-      uint32_t incl = mine;
+      const uint32_t r = r0 + tid, n = wanted<FORK>(a, r, g);
+      uint32_t incl = n;
       for (uint32_t k = 1; k < 64; k *= 2) {
         const uint32_t up = __shfl_up(incl, k);
         if (lane >= k) incl += up;
@@ -184,43 +202,57 @@ __global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
       if (lane == 63) sums[wave] = incl;
       __syncthreads();
       uint32_t before = total;
+      const uint32_t s = lane < kPlanWaves ? sums[lane] : 0;
       for (uint32_t w = 0; w < kPlanWaves; ++w) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
+        const uint32_t x = __builtin_amdgcn_readlane(s, w);
+        if (w < wave) before += x;
+        total += x;
       }
-      if (r < a.n) start[r] = before + incl - mine;
+      at[g] = before + incl - n;
+      mine[g] = n;
+      if (r < a.n) start[r] = at[g];
     }
     if (tid == 0) start[a.n] = total;
     // the lowest free pages
-    const int32_t* refs = a.refs + (uint64_t)g * a.n_pages;
     int32_t* list = a.list + (uint64_t)g * a.n_pages;
     uint32_t have = 0;
     for (uint64_t p0 = 0; p0 < a.n_pages && have < total; p0 += kScan * kPlanThreads) {
+      if (p0) ask(refs, p0);
       uint64_t free[kScan];
-      int32_t held[kScan];
-#pragma unroll
-      for (uint32_t k = 0; k < kScan; ++k) {
-        const uint64_t p = p0 + k * kPlanThreads + tid;
-        held[k] = p < a.n_pages ? refs[p] : 1;
-      }
 #pragma unroll
       for (uint32_t k = 0; k < kScan; ++k) free[k] = __ballot(held[k] <= 0);
-      __syncthreads();  // the last counts have been read
+      __syncthreads();  // the last round's numbers have been read
       if (lane == 0)
 #pragma unroll
-        for (uint32_t k = 0; k < kScan; ++k) cnt[k][wave] = __popcll(free[k]);
+        for (uint32_t k = 0; k < kScan; ++k) before_of[k * kPlanWaves + wave] = __popcll(free[k]);
+      __syncthreads();
+      if (wave == 0) {  // how many there are before each wavefront's of each round
+        constexpr uint32_t kEach = kScan * kPlanWaves / 64;
+        uint32_t n[kEach], sum = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) n[k] = before_of[lane * kEach + k];
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) {
+          const uint32_t x = n[k];
+          n[k] = sum;
+          sum += x;
+        }
+        uint32_t incl = sum;
+        for (uint32_t k = 1; k < 64; k *= 2) {
+          const uint32_t up = __shfl_up(incl, k);
+          if (lane >= k) incl += up;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) before_of[lane * kEach + k] = incl - sum + n[k];
+        if (lane == 63) found_now = incl;
+      }
       __syncthreads();
 #pragma unroll
       for (uint32_t k = 0; k < kScan; ++k) {
-        uint32_t before = have;
-        for (uint32_t w = 0; w < kPlanWaves; ++w) {
-          const uint32_t c = cnt[k][w];
-          if (w < wave) before += c;
-          have += c;
-        }
-        before += lanes_below(free[k]);
-        if ((free[k] >> lane & 1) && before < total) list[before] = (int32_t)(p0 + k * kPlanThreads + tid);
+        const uint32_t i = have + before_of[k * kPlanWaves + wave] + lanes_below(free[k]);
+        if ((free[k] >> lane & 1) && i < total) list[i] = (int32_t)(p0 + k * kPlanThreads + tid);
       }
+      have += found_now;
     }
     if (tid == 0) found[g] = have;
   }
@@ -231,36 +263,46 @@ __global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
     uint8_t said = TL_ACCEPT;
     uint32_t c0 = 0, c1 = 0;
     bool fine = true;
+#pragma unroll
+    for (uint32_t g = 0; g < TL_MAX_GROUPS; ++g) {
+      if (g >= a.n_groups) break;
+      if (!one && r < a.n) {
+        const uint32_t* start = a.start + (uint64_t)g * (a.n + 1);
+        at[g] = start[r];
+        mine[g] = start[r + 1] - at[g];
+      }
+      if (r < a.n && mine[g] && at[g] + mine[g] > found[g]) said = TL_MISSING;
+    }
     if (r < a.n) {
       if constexpr (FORK)
         fine = fork_of(a, r).fine;
       else
         range_of(a, r, c0, c1, fine);
-      for (uint32_t g = 0; g < a.n_groups; ++g) {
-        const uint32_t* start = a.start + (uint64_t)g * (a.n + 1);
-        if (start[r + 1] > start[r] && start[r + 1] > found[g]) said = TL_MISSING;
-      }
       if (!fine) said = TL_BADARG;
       a.served[r] = said;
       if (a.status) a.status[r] = said;
     }
     if constexpr (!FORK) {
       if (said != TL_ACCEPT) c1 = c0;
-      for (uint32_t g = 0; g < a.n_groups; ++g) {
+#pragma unroll
+      for (uint32_t g = 0; g < TL_MAX_GROUPS; ++g) {
+        if (g >= a.n_groups) break;
         const int32_t* list = a.list + (uint64_t)g * a.n_pages;
         int32_t* refs = a.refs + (uint64_t)g * a.n_pages;
         int32_t* row = a.out_tables + ((uint64_t)g * a.n + min(r, a.n - 1)) * a.width;
-        uint32_t at = r < a.n ? a.start[(uint64_t)g * (a.n + 1) + r] : 0;
-        if (c1 - c0 <= kShort)
-          for (uint32_t c = c0; c < c1; ++c)
-            if (row[c] < 0) {
-              const int32_t p = list[at++];
-              row[c] = p;
+        if (c1 - c0 <= kShort) {
+          uint32_t from = at[g];
+#pragma unroll
+          for (uint32_t i = 0; i < kShort; ++i)
+            if (c0 + i < c1 && row[c0 + i] < 0) {
+              const int32_t p = list[from++];
+              row[c0 + i] = p;
               refs[p] = 1;
             }
+        }
         for (uint64_t m = __ballot(c1 - c0 > kShort); m; m &= m - 1) {
           const uint32_t who = (uint32_t)__builtin_ctzll(m), b0 = __shfl(c0, who), b1 = __shfl(c1, who);
-          uint32_t from = __shfl(at, who);
+          uint32_t from = __shfl(at[g], who);
           int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + __shfl(r, who)) * a.width;
           for (uint32_t c = b0; c < b1; c += 64) {
             const bool lacks = c + lane < b1 && theirs[c + lane] < 0;
@@ -320,7 +362,7 @@ __global__ __launch_bounds__(kThreads) void k_pages_fork(ForkArgs a) {
     const uint32_t* start = p.start + (uint64_t)g * (p.n + 1);
     if (p.served[r] != TL_ACCEPT || start[r + 1] == start[r]) continue;
     const Fork f = fork_of(p, r);
-    copy_piece(a.c, slab, last_page(p, f, g), (uint32_t)p.list[(uint64_t)g * p.n_pages + start[r]], f.part, piece);
+    copy_pieces(a.c, slab, last_page(p, f, g), (uint32_t)p.list[(uint64_t)g * p.n_pages + start[r]], f.part, piece, a.pieces);
   }
 }
 
@@ -354,25 +396,28 @@ struct KeepArgs {
   const uint32_t* keep;
   uint32_t* len_out;
   uint8_t* status;
-  uint32_t columns, blocks;  // 16-byte columns of a row, and workgroups that share them
+  uint32_t columns, blocks;  // 16-byte columns of a row, and workgroups (or wavefronts) that share them
+  uint32_t slabs;            // of a wavefront
 };
 
-// The smallest scale byte under which a code (not 0, without its sign) of scale byte
-// `from` is 448 or less: 1.m * 2^e needs 2^(e - 8), twice that above 1.75.
-__device__ __forceinline__ uint32_t scale_for(uint32_t code, uint32_t from) {
-  const uint32_t bits = __float_as_uint(__builtin_amdgcn_cvt_f32_fp8(code, 0));
-  const int b = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0) + (int)from;
-  return (uint32_t)max(b, (int)kScaleMin);
-}
-
-// Largest magnitude among a word's codes that are not NaN.
-__device__ __forceinline__ uint32_t largest_code(uint32_t w, uint32_t m) {
+// Largest magnitude among 16 codes, as values; NaN codes do not count.
+__device__ __forceinline__ float largest_code(u32x4 w) {
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t c = w >> (8 * i) & 0x7f;
-    m = c < 0x7f ? max(m, c) : m;
+  for (int e = 0; e < 4; ++e) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], true);
+    m = fmaxf(fmaxf(fabsf(lo[0]), fabsf(lo[1])), m);
+    m = fmaxf(fmaxf(fabsf(hi[0]), fabsf(hi[1])), m);
   }
   return m;
+}
+
+// The smallest scale byte under which a code's value (above 0) of scale byte `from` is 448
+// or less: 1.m * 2^e needs 2^(e - 8), twice that above 1.75.
+__device__ __forceinline__ uint32_t scale_for(float value, uint32_t from) {
+  const uint32_t bits = __float_as_uint(value);
+  const int b = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0) + (int)from;
+  return (uint32_t)max(b, (int)kScaleMin);
 }
 
 // Codes of scale byte `from`, rounded to scale byte `to`.
@@ -389,81 +434,311 @@ __device__ __forceinline__ u32x4 rescale(u32x4 w, uint32_t from, uint32_t to) {
   return w;
 }
 
-// A workgroup moves C 16-byte columns of one request's rows in one slab, kRows rows
-// at a time with U more behind each. A row only moves towards the front, and never
-// past one that stays: the rows of a step are all read before the first of them is
-// written, and then no later row's source has been written over. So the request's
-// rows are moved in place, in steps that follow each other, and in parallel over
-// columns, slabs and requests.
+// A row only moves towards the front, and never past one that stays: the rows of a step
+// are all read before the first of them is written, and then no later row's source has
+// been written over. So a request's rows are moved in place, in steps that follow each
+// other, and in parallel over columns, slabs and requests.
 //
-// Scaled pages: a step is whole pages of the rows' new places, whose scales follow
-// from the codes' largest magnitudes; a page of more rows than a step holds is read
-// twice.
+// Scaled pages: a step is whole pages of the rows' new places (or all rows that are left),
+// whose scales follow from the codes' largest magnitudes; a page of more rows than a step
+// holds is read twice.
+
+// Rows of one request, and where they go.
+struct Kept {
+  uint32_t rows, before, n, P;
+  bool sound;
+  const uint32_t* keep;
+  const int32_t* table;
+  uint64_t group_stride;
+};
+__device__ __forceinline__ Kept kept_of(const KeepArgs& a, uint32_t r) {
+  Kept k;
+  const uint32_t row0 = a.b.first_row(r), row1 = a.b.first_row(r + 1), kv_len = a.b.kv_len[r];
+  k.rows = row1 > row0 ? row1 - row0 : 0;
+  k.sound = kv_len >= k.rows && kv_len <= a.b.most;
+  k.before = kv_len - k.rows;
+  k.n = k.sound ? min(a.n_keep[r], k.rows) : 0;
+  k.P = a.c.page_tokens;
+  k.keep = a.keep + row0;
+  k.table = a.b.table + (uint64_t)r * a.b.width;
+  k.group_stride = (uint64_t)a.b.n_reqs * a.b.width;
+  return k;
+}
+
+// Rows in front that stay where they are: found by a whole wavefront.
+__device__ __forceinline__ uint32_t rows_in_place(const Kept& k) {
+  const uint32_t lane = threadIdx.x & 63;
+  for (uint32_t i = 0; i < k.n; i += 64) {
+    const uint64_t moves = __ballot(i + lane < k.n && k.keep[min(i + lane, k.n - 1)] != i + lane);
+    if (moves) return i + (uint32_t)__builtin_ctzll(moves);
+  }
+  return k.n;
+}
+
+// Where row i is and where it goes; false: it cannot be kept, since it names no later row
+// than the one before, or has no page in some group (every layer stops at the same row).
+struct RowMove {
+  int64_t from_page, to_page;
+  uint32_t from_row, to_row, page;  // rows of those pages, and the new place's page in the table
+};
+__device__ __forceinline__ bool move_of(const KeepArgs& a, const Kept& k, uint32_t i, uint32_t own, RowMove& m) {
+  const uint32_t at = k.keep[i], last = i ? k.keep[i - 1] : 0;
+  if (at >= k.rows || (i && at <= last)) return false;
+  const uint32_t ps = k.before + at, pd = k.before + i, cs = a.b.page.div(ps), cd = a.b.page.div(pd);
+  bool fine = true;
+  for (uint32_t g = 0; g < a.c.n_groups; ++g) {
+    const uint32_t src = (uint32_t)k.table[g * k.group_stride + cs], dst = (uint32_t)k.table[g * k.group_stride + cd];
+    if (src >= a.c.n_pages || dst >= a.c.n_pages) fine = false;
+    if (g == own) {
+      m.from_page = (int64_t)src * a.c.stride;
+      m.to_page = (int64_t)dst * a.c.stride;
+    }
+  }
+  m.from_row = ps - cs * k.P;
+  m.to_row = pd - cd * k.P;
+  m.page = cd;
+  return fine;
+}
+
+__device__ __forceinline__ void say_kept(const KeepArgs& a, const Kept& k, uint32_t r, uint32_t done, bool bad) {
+  a.len_out[r] = k.sound ? k.before + done : a.b.kv_len[r];
+  if (a.status) a.status[r] = k.sound && !bad && a.n_keep[r] <= k.rows ? TL_ACCEPT : TL_BADARG;
+}
+
+// Few rows: a wavefront by itself takes L 16-byte columns (scaled pages: a head) of one
+// request's rows in some slabs, one after another, and waits for no other. What it costs is
+// instructions and one wait after another, not bytes: so a step's places are found once for
+// all its slabs, a step has as many rows as the lanes hold (accepted drafts are few), and
+// registers are few, for many wavefronts on a SIMD. 96 requests that keep up to 7 of up to 48
+// rows, 32 layers of 8 heads of 128 in 8 bits: 26 us; with 32 rows a step and the next slab's
+// asked for ahead 50 (186 registers and more), a workgroup for all heads and a slab 53. (With
+// 20 of 64 rows kept 125, 85 and - : two steps for each page.)
+template <int L>
+struct FewRows {
+  static constexpr uint32_t R = 64 / L, U = L == 16 ? 2 : 1, N = R * U;  // rows at a time, times, rows of a step
+};
+
+__device__ __forceinline__ int64_t shuffled(int64_t x, uint32_t lane) {
+  const uint32_t lo = __shfl((uint32_t)x, lane), hi = __shfl((uint32_t)((uint64_t)x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// Rows that have been asked for are there, before anything is written after this.
+template <uint32_t U>
+__device__ __forceinline__ void arrived(u32x4 (&x)[U]) {
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]) : : "memory");
+}
+
+template <bool FP8, int L>
+__device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t slab1, uint32_t block) {
+  typedef FewRows<L> F;
+  const uint32_t lane = threadIdx.x & 63, j = lane % L, sub = lane / L, column = block * L + j;
+  const bool there = column < a.columns;
+  const Kept k = kept_of(a, r);
+  const uint32_t own = a.c.group[slab0 >> 1];
+  // the slabs' bases, a lane each: asked for once, and before all else
+  const int64_t bases = (int64_t)a.c.base(min(slab0 + lane, slab1 - 1));
+  uint32_t done = rows_in_place(k);
+  bool bad = false;
+  while (done < k.n && !bad) {
+    const uint32_t pos = k.before + done, page0 = a.b.page.div(pos), o = pos - page0 * k.P;
+    uint32_t ask = k.n - done;  // rows of the step
+    if (ask > F::N) ask = !FP8 ? F::N : (uint32_t)min((uint64_t)ask, ((uint64_t)page0 + (k.P <= F::N ? F::N / k.P : 1)) * k.P - pos);
+    const bool whole = ask <= F::N;  // they are held, not read again
+    const uint32_t last = a.b.page.div(pos + ask - 1);
+    // this lane's rows
+    int64_t from[F::U], to[F::U], from_scale[F::U], to_scale[F::U];
+    uint32_t page[F::U];
+    auto find = [&](uint32_t i, uint32_t count) {
+      RowMove m = {0, 0, 0, 0, 0};
+      const bool fine = lane >= count || move_of(a, k, i + lane, own, m);
+      const uint64_t none = ~__ballot(fine);
+      const int64_t f = m.from_page + (int64_t)m.from_row * a.c.row_bytes, t = m.to_page + (int64_t)m.to_row * a.c.row_bytes;
+#pragma unroll
+      for (uint32_t u = 0; u < F::U; ++u) {
+        const uint32_t at = u * F::R + sub;
+        from[u] = shuffled(f, at) + column * 16;
+        to[u] = shuffled(t, at) + column * 16;
+        if constexpr (FP8) {
+          from_scale[u] = shuffled(m.from_page, at) + a.c.code_bytes + block;
+          to_scale[u] = shuffled(m.to_page, at) + a.c.code_bytes + block;
+          page[u] = __shfl(m.page, at);
+        }
+      }
+      return none ? min(count, (uint32_t)__builtin_ctzll(none)) : count;
+    };
+    int64_t first_scale_at = 0;
+    if (whole) {
+      const uint32_t count = find(done, ask);
+      bad = count < ask;
+      ask = count;
+      if (!ask) break;
+      if constexpr (FP8) first_scale_at = shuffled(to_scale[0], 0);
+    }
+    u32x4 x[F::U] = {};
+    uint32_t scale[F::U] = {};
+#pragma unroll 1
+    for (uint32_t slab = slab0; slab < slab1; ++slab) {
+      const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)bases, slab - slab0);
+      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)((uint64_t)bases >> 32), slab - slab0);
+      const Bytes base = (Bytes)((uint64_t)hi << 32 | lo);
+      auto load = [&](uint32_t count) {
+#pragma unroll
+        for (uint32_t u = 0; u < F::U; ++u)
+          if (u * F::R + sub < count && there) {
+            x[u] = *(Granules)(base + from[u]);
+            if constexpr (FP8) scale[u] = base[from_scale[u]];
+          }
+      };
+      if constexpr (!FP8) {
+        load(ask);
+        arrived(x);
+#pragma unroll
+        for (uint32_t u = 0; u < F::U; ++u)
+          if (u * F::R + sub < ask && there) *(Granules)(base + to[u]) = x[u];
+      } else {
+        uint32_t needs[F::U], first = kScaleMin, old = 0;  // scale bytes of a row's new page, and of the step's first one
+        // what the pages of the rows that were read need
+        auto needs_of = [&](uint32_t count) {
+          uint32_t mine[F::U];
+#pragma unroll
+          for (uint32_t u = 0; u < F::U; ++u) {
+            scale[u] = scale_held(scale[u]);
+            float m = u * F::R + sub < count && there ? largest_code(x[u]) : 0.f;
+#pragma unroll
+            for (int d = 1; d < L; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+            mine[u] = m > 0.f ? scale_for(m, scale[u]) : kScaleMin;
+            needs[u] = kScaleMin;
+          }
+          for (uint32_t p = page0; p <= last; ++p) {  // two pages, mostly
+            uint32_t m = kScaleMin;
+#pragma unroll
+            for (uint32_t u = 0; u < F::U; ++u)
+              if (u * F::R + sub < count && page[u] == p) m = max(m, mine[u]);
+#pragma unroll
+            for (int d = L; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+            if (p == page0) first = max(first, m);
+#pragma unroll
+            for (uint32_t u = 0; u < F::U; ++u)
+              if (page[u] == p) needs[u] = m;
+          }
+        };
+        if (whole) {
+          load(ask);
+          if (o) old = base[first_scale_at];
+          needs_of(ask);
+        } else {
+          for (uint32_t i = 0; i < ask; i += F::N) {
+            const uint32_t want = min(F::N, ask - i), count = find(done + i, want);
+            load(count);
+            if (i == 0) {
+              first_scale_at = shuffled(to_scale[0], 0);
+              if (o && count) old = base[first_scale_at];
+            }
+            needs_of(count);
+            if (count < want) {  // the same for every slab
+              bad = true;
+              ask = i + count;
+            }
+          }
+          if (!ask) break;
+        }
+        if (o) {
+          old = scale_held(old);
+          if (first > old) {  // the page's scale rises: the rows before are rounded again
+            for (uint32_t i = sub; i < o && there; i += F::R) {
+              const Granules at = (Granules)(base + first_scale_at - a.c.code_bytes - block + (int64_t)i * a.c.row_bytes + column * 16);
+              *at = rescale(*at, old, first);
+            }
+          } else {
+            first = old;
+          }
+        }
+        auto store = [&](uint32_t count) {
+          arrived(x);
+#pragma unroll
+          for (uint32_t u = 0; u < F::U; ++u) {
+            if (u * F::R + sub >= count || !there) continue;
+            const uint32_t now = page[u] == page0 ? first : needs[u];
+            *(Granules)(base + to[u]) = scale[u] == now ? x[u] : rescale(x[u], scale[u], now);
+            if (j == 0 && whole) base[to_scale[u]] = (uint8_t)now;  // (each of a page's rows the same)
+          }
+        };
+        if (whole) {
+          store(ask);
+        } else {
+          for (uint32_t i = 0; i < ask; i += F::N) {
+            const uint32_t count = find(done + i, min(F::N, ask - i));
+            load(count);
+#pragma unroll
+            for (uint32_t u = 0; u < F::U; ++u) scale[u] = scale_held(scale[u]);
+            store(count);
+          }
+          if (there && j == 0 && sub == 0) base[first_scale_at] = (uint8_t)first;  // no row asks for the one before any more
+        }
+      }
+    }
+    done += ask;
+  }
+  if (slab0 == 0 && block == 0 && lane == 0) say_kept(a, k, r, done, bad);
+}
+
+template <bool FP8, int L>
+__global__ __launch_bounds__(kThreads) void k_keep_few(KeepArgs a) {
+  const uint64_t per = (uint64_t)((a.c.n_slabs + a.slabs - 1) / a.slabs) * a.blocks, items = a.b.n_reqs * per;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  for (uint64_t item = (uint64_t)blockIdx.x * (kThreads / 64) + wave; item < items; item += (uint64_t)gridDim.x * (kThreads / 64)) {
+    const uint32_t rest = (uint32_t)(item % per), slab0 = rest / a.blocks * a.slabs;
+    keep_few<FP8, L>(a, (uint32_t)(item / per), slab0, min(slab0 + a.slabs, a.c.n_slabs), rest % a.blocks);
+  }
+}
+
+// Many rows: bounded by memory. A workgroup takes C 16-byte columns of a slab, kRows rows
+// at a time with U more behind each.
 template <bool FP8, int C, int U>
 struct KeepLds {
   static constexpr uint32_t R = kThreads / C, N = R * U;  // rows at a time, rows of a step
   int64_t from[N], to[N];                                 // bytes from a slab's start
-  uint32_t first_bad, first_move;
-  uint32_t slot[FP8 ? N : 1];               // a row's new page, among the step's
-  uint32_t need[FP8 ? N : 1][FP8 ? C / 4 : 1];  // scale bytes of those pages, of the workgroup's heads
+  int64_t from_page[FP8 ? N : 1], to_page[FP8 ? N : 1];
+  uint32_t good[kThreads / 64];                           // of each wavefront's rows
+  uint32_t slot[FP8 ? N : 1];                             // a row's new page, among the step's
+  uint32_t need[FP8 ? N : 1][FP8 ? C / 4 : 1];            // scale bytes of those pages, of the workgroup's heads
 };
 
 template <bool FP8, int C, int U>
-__device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, uint32_t slab, uint32_t block) {
+__device__ void keep_many(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, uint32_t slab, uint32_t block) {
   constexpr uint32_t R = kThreads / C, N = R * U;
-  const uint32_t tid = threadIdx.x, col = tid % C, sub = tid / C, column = block * C + col;
+  static_assert(N <= kThreads, "a thread for each row of a step");
+  const uint32_t tid = threadIdx.x, lane = tid & 63, col = tid % C, sub = tid / C, column = block * C + col;
   const bool there = column < a.columns;
-  const uint32_t row0 = a.b.first_row(r), row1 = a.b.first_row(r + 1), rows = row1 > row0 ? row1 - row0 : 0;
-  const uint32_t kv_len = a.b.kv_len[r], asked = a.n_keep[r], P = a.c.page_tokens;
-  const bool sound = kv_len >= rows && kv_len <= a.b.most;
-  const uint32_t before = kv_len - rows, n = sound ? min(asked, rows) : 0;
-  const uint32_t* keep = a.keep + row0;
+  const Kept k = kept_of(a, r);
   const uint32_t own = a.c.group[slab >> 1];
   const Bytes base = (Bytes)a.c.base(slab);
-  const uint64_t group_stride = (uint64_t)a.b.n_reqs * a.b.width;
-  const int32_t* table = a.b.table + (uint64_t)r * a.b.width;
+  uint32_t done = rows_in_place(k), page0 = 0;  // page0: the step's first page
 
-  // rows in front that stay where they are
-  uint32_t done = 0;
-  for (bool more = true; more && done < n;) {
-    __syncthreads();
-    if (tid == 0) l.first_move = ~0u;
-    __syncthreads();
-    const uint32_t i = done + tid;
-    if (i < n && keep[i] != i) atomicMin(&l.first_move, i);
-    __syncthreads();
-    more = l.first_move == ~0u;
-    done = more ? min(n, done + kThreads) : l.first_move;
-  }
-
-  // The places of rows [i, i + count), and how many of them can be kept: up to the
-  // first that names no later row, or has no page in some group: every layer stops
-  // at the same row.
-  uint32_t page0 = 0;  // the step's first page
+  // The places of rows [i, i + count), and how many of them can be kept.
   auto find = [&](uint32_t i, uint32_t count) {
     __syncthreads();  // what was found last has been used
-    if (tid == 0) l.first_bad = ~0u;
-    __syncthreads();
-    for (uint32_t t = tid; t < count; t += kThreads) {
-      const uint32_t k = keep[i + t], last = i + t ? keep[i + t - 1] : 0;
-      bool fine = k < rows && (i + t == 0 || k > last);
-      if (fine) {
-        const uint32_t ps = before + k, pd = before + i + t;
-        const uint32_t cs = a.b.page.div(ps), cd = a.b.page.div(pd);
-        for (uint32_t g = 0; g < a.c.n_groups; ++g) {
-          const uint32_t src = (uint32_t)table[g * group_stride + cs], dst = (uint32_t)table[g * group_stride + cd];
-          if (src >= a.c.n_pages || dst >= a.c.n_pages) fine = false;
-          if (g == own) {
-            l.from[t] = (int64_t)src * a.c.stride + (int64_t)(ps - cs * P) * a.c.row_bytes;
-            l.to[t] = (int64_t)dst * a.c.stride + (int64_t)(pd - cd * P) * a.c.row_bytes;
-          }
-        }
-        if constexpr (FP8) l.slot[t] = cd - page0;
+    bool fine = true;
+    if (tid < count) {
+      RowMove m = {0, 0, 0, 0, 0};
+      fine = move_of(a, k, i + tid, own, m);
+      l.from[tid] = m.from_page + (int64_t)m.from_row * a.c.row_bytes;
+      l.to[tid] = m.to_page + (int64_t)m.to_row * a.c.row_bytes;
+      if constexpr (FP8) {
+        l.from_page[tid] = m.from_page;
+        l.to_page[tid] = m.to_page;
+        l.slot[tid] = m.page - page0;
       }
-      if (!fine) atomicMin(&l.first_bad, t);
     }
+    const uint64_t bad = ~__ballot(fine);
+    if (lane == 0) l.good[tid / 64] = bad ? tid + (uint32_t)__builtin_ctzll(bad) : ~0u;
     __syncthreads();
-    return min(count, l.first_bad);
+    uint32_t good = count;
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 64; ++w) good = min(good, l.good[w]);
+    return good;
   };
 
   bool bad = false;
@@ -474,9 +749,9 @@ __device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, 
       if (there && u * R + sub < count) x[u] = *(Granules)(base + l.from[u * R + sub] + column * 16);
   };
   if constexpr (!FP8) {
-    while (done < n && !bad) {
-      const uint32_t ask = min(N, n - done), count = find(done, ask);
-      bad = count < ask;
+    while (done < k.n && !bad) {
+      const uint32_t want = min(N, k.n - done), count = find(done, want);
+      bad = count < want;
       load(count);
       __syncthreads();  // all of the step's rows are read
 #pragma unroll
@@ -488,45 +763,37 @@ __device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, 
     const uint32_t lanes = a.c.row_bytes / a.c.n_scales / 16;  // of a head
     const uint32_t head = min(column / lanes, a.c.n_scales - 1), mine = col / lanes;
     const bool leads = there && col % lanes == 0;
-    while (done < n && !bad) {
-      const uint32_t pos = before + done;
+    while (done < k.n && !bad) {
+      const uint32_t pos = k.before + done;
       page0 = a.b.page.div(pos);
-      const uint32_t o = pos - page0 * P;  // of the first page, rows before
-      const uint64_t end = ((uint64_t)page0 + (P <= N ? N / P : 1)) * P;
-      uint32_t ask = (uint32_t)min((uint64_t)(n - done), end - pos);
+      const uint32_t o = pos - page0 * k.P;  // of the first page, rows before
+      const uint64_t end = k.n - done <= N ? ~0ull : ((uint64_t)page0 + (k.P <= N ? N / k.P : 1)) * k.P;
+      uint32_t ask = (uint32_t)min((uint64_t)(k.n - done), end - pos);
       const bool whole = ask <= N;  // the rows are held, not read again
       uint32_t scale[U];
-      auto load_scales = [&](uint32_t i, uint32_t count) {
+      auto load_scales = [&](uint32_t count) {
 #pragma unroll
-        for (uint32_t u = 0; u < U; ++u) {
-          const uint32_t t = u * R + sub;
-          if (t >= count) continue;
-          const uint32_t at = before + keep[i + t];
-          const int64_t page = l.from[t] - (int64_t)(at - a.b.page.div(at) * P) * a.c.row_bytes;
-          scale[u] = scale_held(base[page + a.c.code_bytes + head]);
-        }
+        for (uint32_t u = 0; u < U; ++u)
+          if (u * R + sub < count) scale[u] = scale_held(base[l.from_page[u * R + sub] + a.c.code_bytes + head]);
       };
       __syncthreads();
       for (uint32_t t = tid; t < N * (C / 4); t += kThreads) l.need[t / (C / 4)][t % (C / 4)] = kScaleMin;
       int64_t first_page = 0;
-      for (uint32_t s = 0; s < ask; s += N) {
-        const uint32_t want = min(N, ask - s), count = find(done + s, want);
-        if (s == 0 && count) first_page = l.to[0] - (int64_t)o * a.c.row_bytes;
+      for (uint32_t i = 0; i < ask; i += N) {
+        const uint32_t want = min(N, ask - i), count = find(done + i, want);
+        if (i == 0 && count) first_page = l.to_page[0];
         load(count);
-        load_scales(done + s, count);
+        load_scales(count);
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
           const uint32_t t = u * R + sub;
-          uint32_t m = 0;
-          if (there && t < count)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m = largest_code(x[u][e], m);
-          for (uint32_t k = 1; k < lanes; k *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, k));
-          if (leads && m) atomicMax(&l.need[l.slot[t]][mine], scale_for(m, scale[u]));
+          float m = there && t < count ? largest_code(x[u]) : 0.f;
+          for (uint32_t d = 1; d < lanes; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+          if (leads && m > 0.f) atomicMax(&l.need[l.slot[t]][mine], scale_for(m, scale[u]));
         }
         if (count < want) {
           bad = true;
-          ask = s + count;
+          ask = i + count;
         }
       }
       __syncthreads();  // all rows are read (or will be again), and what their pages need is known
@@ -543,7 +810,7 @@ __device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, 
           first_scale = old;
         }
       }
-      auto store = [&](uint32_t i, uint32_t count) {
+      auto store = [&](uint32_t count) {
 #pragma unroll
         for (uint32_t u = 0; u < U; ++u) {
           const uint32_t t = u * R + sub;
@@ -551,22 +818,20 @@ __device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, 
           const uint32_t to = l.slot[t] ? l.need[l.slot[t]][mine] : first_scale;
           *(Granules)(base + l.to[t] + column * 16) = scale[u] == to ? x[u] : rescale(x[u], scale[u], to);
           // a page's scale, with the first of its rows that move
-          if (whole && leads && (t == 0 || l.slot[t] != l.slot[t - 1])) {
-            const uint32_t at = before + i + t;
-            base[l.to[t] - (int64_t)(at - a.b.page.div(at) * P) * a.c.row_bytes + a.c.code_bytes + head] = (uint8_t)to;
-          }
+          if (whole && leads && (t == 0 || l.slot[t] != l.slot[t - 1])) base[l.to_page[t] + a.c.code_bytes + head] = (uint8_t)to;
         }
       };
       if (whole) {
-        store(done, ask);
+        __syncthreads();  // the first page's scale before has been read
+        store(ask);
       } else {
-        for (uint32_t s = 0; s < ask; s += N) {
-          const uint32_t count = min(N, ask - s);
-          find(done + s, count);
+        for (uint32_t i = 0; i < ask; i += N) {
+          const uint32_t count = min(N, ask - i);
+          find(done + i, count);
           load(count);
-          load_scales(done + s, count);
+          load_scales(count);
           __syncthreads();  // all of these rows are read
-          store(done + s, count);
+          store(count);
         }
         __syncthreads();  // no row asks for the scale before any more
         if (leads && sub == 0) base[first_page + a.c.code_bytes + head] = (uint8_t)first_scale;
@@ -574,10 +839,7 @@ __device__ void keep_rows(const KeepArgs& a, KeepLds<FP8, C, U>& l, uint32_t r, 
       done += ask;
     }
   }
-  if (slab == 0 && block == 0 && tid == 0) {
-    a.len_out[r] = sound ? before + done : kv_len;
-    if (a.status) a.status[r] = sound && !bad && asked <= rows ? TL_ACCEPT : TL_BADARG;
-  }
+  if (slab == 0 && block == 0 && tid == 0) say_kept(a, k, r, done, bad);
 }
 
 template <bool FP8, int C, int U>
@@ -586,7 +848,7 @@ __global__ __launch_bounds__(kThreads) void k_keep(KeepArgs a) {
   const uint64_t per = (uint64_t)a.c.n_slabs * a.blocks, items = a.b.n_reqs * per;
   for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const uint32_t rest = (uint32_t)(item % per);
-    keep_rows<FP8, C, U>(a, l, (uint32_t)(item / per), rest / a.blocks, rest % a.blocks);
+    keep_many<FP8, C, U>(a, l, (uint32_t)(item / per), rest / a.blocks, rest % a.blocks);
   }
 }
 
@@ -604,6 +866,15 @@ void fill_slabs(Slabs& s, const tl_ctx* ctx, const tl_cache* c) {
   s.n_scales = scaled ? ctx->H : 0;
   s.n_groups = ctx->geo.n_groups;
   std::copy(ctx->geo.group, ctx->geo.group + ctx->L, s.group);
+}
+
+// Workgroups of each of `copies` pages: one for 64 KiB where that fills the device, else one
+// for each piece. us, 301 pages of 64 KiB, about half of each, 24 slabs: 107 with one, 116 with
+// four (whole pages 193 and 194); 30 of 1 MiB: 182 with one, 155 with 64; 8 pages of 4 slabs 4.7
+// and 3.8.
+uint32_t pieces_of(uint32_t bytes, uint64_t copies) {
+  const uint32_t wide = (bytes + 4 * kPiece - 1) / (4 * kPiece);
+  return copies * wide >= 2048 ? wide : (bytes + kPiece - 1) / kPiece;
 }
 
 uint32_t grid_of(uint64_t items) { return (uint32_t)std::min<uint64_t>(items, kMostGroups); }
@@ -649,7 +920,7 @@ int launch_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, ui
   a.dst = d_dst;
   a.rows = d_rows;
   a.n = (uint32_t)n;
-  a.pieces = pieces_of(a.c.code_bytes);
+  a.pieces = pieces_of(a.c.code_bytes, n * a.c.n_slabs);
   (void)hipGetLastError();
   {
     TimedLaunch timed(TL_KERNEL_PAGES, stream);
@@ -670,7 +941,7 @@ int launch_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, cons
   a.p.n_parents = (uint32_t)n_parents;
   a.p.out_tables = d_tables_out;
   a.p.out_len = d_len_out;
-  a.pieces = pieces_of(a.c.code_bytes);
+  a.pieces = pieces_of(a.c.code_bytes, n * a.c.n_slabs);
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
   {
@@ -723,23 +994,36 @@ int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const ui
   a.status = d_status;
   a.columns = a.c.row_bytes / 16;
   const bool many = batch->n_rows / batch->n_reqs > 256;
-  const uint32_t C = many ? 16 : 64;
-  a.blocks = (a.columns + C - 1) / C;
-  const dim3 grid(grid_of((uint64_t)batch->n_reqs * a.c.n_slabs * a.blocks));
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
   {
     TimedLaunch timed(TL_KERNEL_KEEP, stream);
-    if (ctx->dtype == TL_DTYPE_FP8_SCALED) {
-      if (many)
+    const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED;
+    if (many) {
+      a.blocks = (a.columns + 15) / 16;
+      const dim3 grid(grid_of((uint64_t)batch->n_reqs * a.c.n_slabs * a.blocks));
+      if (fp8)
         hipLaunchKernelGGL((k_keep<true, 16, 8>), grid, dim3(kThreads), 0, s, a);
       else
-        hipLaunchKernelGGL((k_keep<true, 64, 4>), grid, dim3(kThreads), 0, s, a);
-    } else {
-      if (many)
         hipLaunchKernelGGL((k_keep<false, 16, 8>), grid, dim3(kThreads), 0, s, a);
+    } else {
+      const uint32_t L = fp8 ? ctx->D / 16 : 8;
+      a.blocks = (a.columns + L - 1) / L;
+      // A wavefront's slabs, of one group of layers (a layer's two, or any): as many as leave
+      // work for six wavefronts on every SIMD, up to 8. us with 2 / 4 / 8 / 16: 96 requests of 64
+      // slabs of 8 heads 30 / 26 / 24 / 31, 8 of them 7.1 / 9.3 / 14 / 23.
+      const uint64_t all = (uint64_t)batch->n_reqs * a.c.n_slabs * a.blocks;
+      a.slabs = a.c.n_groups == 1 ? (uint32_t)std::clamp<uint64_t>(all / 6144 & ~1ull, 2, 8) : 2;
+      const uint64_t items = (uint64_t)batch->n_reqs * ((a.c.n_slabs + a.slabs - 1) / a.slabs) * a.blocks;
+      const dim3 grid(grid_of((items + kThreads / 64 - 1) / (kThreads / 64)));
+      if (!fp8)
+        hipLaunchKernelGGL((k_keep_few<false, 8>), grid, dim3(kThreads), 0, s, a);
+      else if (L == 4)
+        hipLaunchKernelGGL((k_keep_few<true, 4>), grid, dim3(kThreads), 0, s, a);
+      else if (L == 8)
+        hipLaunchKernelGGL((k_keep_few<true, 8>), grid, dim3(kThreads), 0, s, a);
       else
-        hipLaunchKernelGGL((k_keep<false, 64, 4>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_keep_few<true, 16>), grid, dim3(kThreads), 0, s, a);
     }
   }
   return launched();

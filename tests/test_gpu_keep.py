@@ -73,6 +73,18 @@ def test_drafts(cache, P, H, D, layers, group_of, pad, spread):
     assert lens == want[0] and status == want[1] and set(status) == {T.ACCEPT}
 
 
+@pytest.mark.parametrize("cache,requests", [("bf16", 40), ("fp8_scaled", 40), ("fp8_scaled", 66)])
+def test_many_slabs(cache, requests):
+    """So much work that a wavefront takes several layers, 4 or 8 slabs of them."""
+    r = np.random.default_rng(9)
+    new = r.integers(1, 12, requests).tolist()
+    kv_len = [a + int(h) for a, h in zip(new, r.integers(0, 40, requests))]
+    kept = [some(r, n, int(r.integers(0, min(n, 4) + 1))) for n in new]
+    c, tables = make(10, 16, 16, 64, cache, new, kv_len, layers=25)
+    lens, status, want = run(c, tables, new, kv_len, kept)
+    assert lens == want[0] and status == want[1]
+
+
 @pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
 @pytest.mark.parametrize("P,H,D,layers,group_of,pad", FEW)
 def test_many_rows(cache, P, H, D, layers, group_of, pad):
