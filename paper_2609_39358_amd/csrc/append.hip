@@ -483,8 +483,10 @@ __device__ void put_row(const AppendArgs& a, uint32_t t) {
       const bool is_v = !FP8 && u >= nq + H;
       float x[16];
       Weights w;
-      if constexpr (NORM)
-        if (!is_v) w = load_weights(a, u >= nq, u >= nq ? u - nq : u, first, second);
+      if constexpr (NORM) {
+        const bool is_k = !FP8 && u >= nq;
+        if (!is_v) w = load_weights(a, is_k, is_k ? u - nq : u, first, second);
+      }
       values<D, NORM>(a, raw[i], !is_v, j, g, &w, x);
       GlobalOut out = (GlobalOut)(a.q_out + (int64_t)t * a.qo_token + (int64_t)u * a.qo_head);
       if (!FP8 && u >= nq) {
@@ -501,7 +503,7 @@ __device__ void put_row(const AppendArgs& a, uint32_t t) {
 // of K and V each: those fragments (rows of one request that go to one scaled page)
 // that begin there. The others take a row per wavefront.
 template <int D, int HELD, bool NORM>
-__global__ __launch_bounds__(64 * kWaves) void k_append(AppendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, NORM && HELD == 2 ? 2 : 1) void k_append(AppendArgs a) {
   constexpr bool FP8 = HELD > 0;
   uint32_t block = blockIdx.x;
   if constexpr (FP8) {
@@ -552,6 +554,8 @@ void launch(bool fp8, uint32_t grid, hipStream_t s, const AppendArgs& a) {
     // windows, four do. 24,573 tokens into pages of 16 rows of 16 heads of 128: 153 us,
     // 4.7 TB/s, with two rows held 170; 64 requests of 2 rows 7.6 and 9.5; 128
     // windows of 16 rows 17.7 and 14.9.
+    // (With norms 24,573 tokens take 190 to 210 us, 40 more registers; in bf16 pages, a row a
+    // wavefront, 167 to 187, where 811 MB at a large copy's rate take 174.)
     hipLaunchKernelGGL((k_append<D, 1, NORM>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   else
     hipLaunchKernelGGL((k_append<D, 2, NORM>), dim3(grid), dim3(64 * kWaves), 0, s, a);
@@ -634,6 +638,13 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     a.splits = a.step > 1 && a.n_windows < many ? std::min((many + a.n_windows - 1) / a.n_windows, (ctx->H + kWaves - 1) / kWaves) : 1;
     a.split_heads = (ctx->H + a.splits - 1) / a.splits;
     a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
+    // Fragments that begin in one window are written one after another, so few windows are made
+    // shorter. us before and after, 8 heads of 128 on pages of 16 rows: 96 requests of 24 rows 22 and
+    // 18 (with norms 36 and 25), 16 of up to 24 rows 16 and 10; 384 windows would take 47 for 40.
+    while (a.step > 2 && a.n_windows < 256) {
+      a.step = (a.step + 1) / 2;
+      a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
+    }
   }
   const uint32_t single = !fp8 || q || d_status ? (a.b.n_rows + kWaves - 1) / kWaves : 0;
   const uint32_t grid = a.n_windows * a.splits + single;
