@@ -375,17 +375,23 @@ class NewTokens:
     included), d_tables i32 [n_groups, n, width] (each request's pages in order:
     the restored ones, then fresh ones), d_cos_sin f32 [positions, rot / 2, 2] or
     None for keys and queries that are not rotated. One workspace serves all
-    layers; `status` has layer()'s verdict per row (valid after the stream syncs)."""
+    layers; `status` has layer()'s verdict per row (valid after the stream syncs).
+
+    Drafted tokens: with d_seen i64 [n_rows, words] the rows of a request are a tree
+    and see each other by their masks (tl_tree), and d_pos i32 [n_rows] are their
+    positions, for the rotation and for windows. keep() moves the accepted ones
+    together once all layers are done."""
 
     def __init__(self, ctx: T.Ctx, cache: PagedCache, n_q_heads: int, n_rows: int, d_row_off, d_kv_len, d_tables,
-                 d_cos_sin=None, stream=None):
+                 d_cos_sin=None, stream=None, d_seen=None, d_pos=None):
         self.ctx, self.n_rows, self.n_q_heads = ctx, n_rows, n_q_heads
         self.stream = stream or torch.cuda.current_stream()
         n, width = d_kv_len.shape[0], d_tables.shape[-1]
         self.cache, self._pages = cache.tl(), cache
         self.batch = T.make_batch(n, n_rows, d_row_off, d_kv_len, d_tables, width)
-        self.rope = None if d_cos_sin is None else T.make_rope(d_cos_sin, 2 * d_cos_sin.shape[1])
-        self._outlive(d_row_off, d_kv_len, d_tables, d_cos_sin)
+        self.rope = None if d_cos_sin is None else T.make_rope(d_cos_sin, 2 * d_cos_sin.shape[1], d_pos)
+        self.tree = None if d_seen is None else T.make_tree(d_seen, d_pos)
+        self._outlive(d_row_off, d_kv_len, d_tables, d_cos_sin, d_seen, d_pos)
         dev = cache.k[0].device
         with _on(self.stream):
             self.ws_bytes = T.tl_attend_workspace_bytes(ctx, n_q_heads, n, n_rows)
@@ -400,14 +406,88 @@ class NewTokens:
                 if x is not None:
                     x.record_stream(self.stream)
 
-    def layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor = None) -> torch.Tensor:
+    def layer(self, l: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lse: torch.Tensor = None,
+              norm: T.tl_norm = None) -> torch.Tensor:
         """q [n_rows, n_q_heads, D], k and v [n_rows, n_kv_heads, D] in bf16, as
-        the model's projections left them (slices of one tensor will do). Returns
-        [n_rows, n_q_heads, D]."""
+        the model's projections left them (slices of one tensor will do); norm: the
+        layer's norms of queries and keys (make_norm). Returns [n_rows, n_q_heads, D]."""
         s = self.stream
-        self._outlive(q, k, v, lse)
+        self._outlive(q, k, v, lse, *(getattr(norm, "_keep", ())))
         with _on(s):
             out = torch.empty_like(self.q)
-            T.tl_append(self.ctx, s, l, self.batch, self.cache, k, v, self.rope, q, self.q, self.status)
-            T.tl_attend(self.ctx, s, l, self.batch, self.cache, self.q, out, self.ws, self.ws_bytes, lse=lse)
+            T.tl_append(self.ctx, s, l, self.batch, self.cache, k, v, self.rope, q, self.q, self.status, norm)
+            T.tl_attend(self.ctx, s, l, self.batch, self.cache, self.q, out, self.ws, self.ws_bytes, lse=lse, tree=self.tree)
         return out
+
+    def keep(self, d_n_keep, d_keep) -> torch.Tensor:
+        """The rows that stay, in every layer: request i's row d_keep[d_row_off[i] + j]
+        of its new ones becomes its new row j, j < d_n_keep[i] (u32, ascending). Returns
+        the requests' lengths after it, u32 [n]; `kept` has a verdict for each."""
+        s, n = self.stream, self.batch.n_reqs
+        self._outlive(d_n_keep, d_keep)
+        with _on(s):
+            lens = torch.empty(n, dtype=torch.int32, device=self.q.device)
+            self.kept = torch.empty(n, dtype=torch.uint8, device=self.q.device)
+            T.tl_keep(self.ctx, s, self.batch, self.cache, d_n_keep, d_keep, lens, self.kept)
+        return lens
+
+
+class PagePool:
+    """Whose a cache's pages are, for engines that keep that on the device: requests
+    take pages, branch (sharing what they have in common) and give them back, with no
+    host step in between. `refs` i32 [n_groups, n_pages] counts each page's owners;
+    `used` lists pages that are never given out. Tables are i32 [n_groups, n, width]
+    with -1 where a request has no page; `status` has the verdicts of the last take()
+    or fork() (valid after the stream syncs)."""
+
+    def __init__(self, ctx: T.Ctx, cache: PagedCache, used=(), stream=None):
+        self.ctx, self.cache, self._pages = ctx, cache.tl(), cache
+        self.stream = stream or torch.cuda.current_stream()
+        dev = cache.k[0].device
+        refs = torch.zeros((ctx.n_groups, cache.n_pages), dtype=torch.int32)
+        refs[:, list(used)] = 1
+        with _on(self.stream):
+            self.refs = refs.to(dev)
+            self.pool = T.make_pool(self.refs)
+        self.status = None
+
+    def _outlive(self, *arrays):
+        """The caller may drop them before the stream has read them."""
+        if self.stream != torch.cuda.current_stream():
+            for x in arrays:
+                if x is not None:
+                    x.record_stream(self.stream)
+
+    def _scratch(self, n: int):
+        """A call's workspace and verdicts, on its stream."""
+        size = T.tl_pages_workspace_bytes(self.ctx, n, self.pool.n_pages)
+        with torch.cuda.stream(self.stream):
+            self.status = torch.empty(n, dtype=torch.uint8, device=self.refs.device)
+            return torch.empty(size, dtype=torch.uint8, device=self.refs.device), size
+
+    def take(self, d_have, d_want, d_tables):
+        """Pages for the tokens [d_have[i], d_want[i]) of every request, into d_tables."""
+        n, width = d_tables.shape[1:]
+        self._outlive(d_have, d_want, d_tables)
+        ws, size = self._scratch(n)
+        with _on(self.stream):
+            T.tl_pages_take(self.ctx, self.stream, self.pool, n, d_have, d_want, d_tables, width, ws, size, self.status)
+
+    def fork(self, d_kv_len, d_tables, d_parent):
+        """Branches of the requests d_parent: their tables [n_groups, n, width] and lengths [n]."""
+        (groups, parents, width), n = d_tables.shape, d_parent.shape[0]
+        self._outlive(d_kv_len, d_tables, d_parent)
+        ws, size = self._scratch(n)
+        with _on(self.stream):
+            tables = torch.empty((groups, n, width), dtype=torch.int32, device=self.refs.device)
+            lens = torch.empty(n, dtype=torch.int32, device=self.refs.device)
+            T.tl_pages_fork(self.ctx, self.stream, self.pool, self.cache, parents, d_kv_len, d_tables, n, d_parent, lens, tables,
+                            width, ws, size, self.status)
+        return tables, lens
+
+    def free(self, d_tables, d_first=None, d_end=None):
+        """Gives back what the tables name (within tokens [d_first[i], d_end[i]), if given)."""
+        n, width = d_tables.shape[1:]
+        self._outlive(d_tables, d_first, d_end)
+        with _on(self.stream):
+            T.tl_pages_free(self.ctx, self.stream, self.pool, n, d_tables, width, d_first, d_end)

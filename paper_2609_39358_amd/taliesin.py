@@ -95,17 +95,17 @@ class tl_pool(ctypes.Structure):
 
 
 # torch's types of the operators' arguments, where torch is there
-_BF16 = None
+_BF16 = _I32 = None
 _WORDS = _LONGS = _FLOATS = _BYTES = ()
 
 
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError("libtaliesin.so is not built (python -m paper_2609_39358_amd.build)")
-    global _BF16, _WORDS, _LONGS, _FLOATS, _BYTES
+    global _BF16, _I32, _WORDS, _LONGS, _FLOATS, _BYTES
     try:  # bind the library's HIP calls to the runtime torch has already loaded
         import torch
-        _BF16 = torch.bfloat16
+        _BF16, _I32 = torch.bfloat16, torch.int32
         _WORDS, _FLOATS = (torch.int32, torch.uint32, torch.uint8), (torch.float32,)
         _LONGS = (torch.int64, torch.uint64)
         _BYTES = (torch.uint8, torch.int8, torch.bool)
@@ -790,12 +790,18 @@ def _check_pool(ctx: Ctx, pool: tl_pool):
 
 
 def _words(x, n: int, what: str):
+    if x is None:
+        return None
+    if getattr(x, "dtype", None) is _I32 and x.is_cuda and x.is_contiguous() and x.numel() >= n:
+        return x.data_ptr()  # (these calls are small: their checks are what they cost)
     _of_type(x, _WORDS, what)
     _fits(x, 4 * n, what)
     return _addr(x)
 
 
 def _status(x, n: int):
+    if x is None:
+        return None
     _of_type(x, _BYTES, "status")
     _fits(x, n, "status")
     return _addr(x)
