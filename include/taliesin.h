@@ -687,8 +687,8 @@ size_t tl_pages_workspace_bytes(const tl_ctx* ctx, size_t n, size_t n_pages);
  * pages a row's values are written as tl_append writes them (from the first row on that
  * moves): a code is moved as it is where the scales agree, and rounded again where they
  * do not. What lies behind the last kept token is not defined. Pages that a kept token
- * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs], not
- * overlapping d_kv_len) becomes the request's length. d_status (device [n_reqs] or NULL):
+ * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs], apart
+ * from the arrays that are read) becomes the request's length. d_status (device [n_reqs] or NULL):
  * TL_ACCEPT, or TL_BADARG where an entry is not larger than the one before, names no new
  * token, or needs a page that the tables do not name: the tokens before that entry are
  * kept, in all layers, and d_len_out says how many; or where d_kv_len is less than the

@@ -251,8 +251,9 @@ int tl_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32
   if (!batch->n_reqs) return TL_OK;
   if (!words_ok(batch->d_row_off) || !words_ok(batch->d_kv_len)) return TL_EINVAL;
   if (!words_ok(d_n_keep) || !words_ok(d_len_out) || (batch->n_rows && !words_ok(d_keep))) return TL_EINVAL;
-  if (overlap(d_len_out, 4 * batch->n_reqs, batch->d_kv_len, 4 * batch->n_reqs) ||
-      overlap(d_len_out, 4 * batch->n_reqs, d_n_keep, 4 * batch->n_reqs))
+  const uint64_t lens = 4 * batch->n_reqs;
+  if (overlap(d_len_out, lens, batch->d_kv_len, lens) || overlap(d_len_out, lens, d_n_keep, lens) ||
+      overlap(d_len_out, lens, batch->d_row_off, lens + 4) || overlap(d_len_out, lens, d_keep, 4 * batch->n_rows))
     return TL_EINVAL;
   return tl::launch_keep(ctx, stream, batch, d_n_keep, d_keep, cache, d_len_out, d_status);
 }

@@ -141,3 +141,66 @@ def test_no_requests_and_no_rows():
     c, tables = make(7, 16, 4, 64, "bf16", [2], [2])
     lens, status, want = run(c, np.repeat(tables, 2, 1), [0, 0], [0, 5], [[], []])
     assert lens == [0, 5] and status == [T.ACCEPT, T.ACCEPT]
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
+@pytest.mark.parametrize("long", [False, True])
+def test_captured_on_a_stream_of_its_own(cache, long):
+    """Replayed with other entries, lengths and tables; every replay against the host."""
+    r = np.random.default_rng(11)
+    new = [700, 40] if long else [12, 7]
+    kv_len = [a + 21 for a in new]
+    c, tables = make(12, 16, 4, 64, cache, new, kv_len)
+    off = np.concatenate([[0], np.cumsum(new)])
+    d_keep, d_n, d_len, d_tab = up(np.zeros(sum(new))), up(np.zeros(2)), up(np.array(kv_len)), up(tables)
+    batch, pages = T.make_batch(2, sum(new), up(off), d_len, d_tab, tables.shape[2]), c.paged.tl()
+    out, status = up(np.zeros(2)), torch.zeros(2, dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        T.tl_keep(c.ctx, side, batch, pages, d_n, d_keep, out, status)
+    for turn in range(4):
+        kept = [some(r, n, int(r.integers(1, n // 2))) for n in new]
+        kv = [k - int(r.integers(0, 5)) for k in kv_len]
+        flat = np.zeros(sum(new), np.int64)
+        for i, k in enumerate(kept):
+            flat[off[i]:off[i] + len(k)] = k
+        # the other order of each request's pages behind its first
+        for g in range(c.groups):
+            for i in range(2):
+                at = np.flatnonzero(tables[g, i] >= 0)
+                tables[g, i, at[1:]] = tables[g, i, at[1:]][::-1]
+        for x, y in ((d_keep, flat), (d_n, np.array([len(k) for k in kept])), (d_len, np.array(kv)), (d_tab, tables)):
+            x.copy_(up(y))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = hc.keep(c, tables, new, kv, kept)
+        assert out.tolist() == want[0] and status.tolist() == want[1], turn
+        c.same("replay %d" % turn)
+
+
+@pytest.mark.parametrize("long", [False, True])
+def test_offsets_past_32_bits(long):
+    """Pages beyond the first 4 GiB of a cache."""
+    from paper_2609_39358_amd.device import PagedCache
+
+    r = np.random.default_rng(13)
+    new = [600] if long else [20]
+    kept = [some(r, new[0], new[0] // 3)]
+    c, tables = make(14, 16, 8, 128, "fp8_scaled", new, [new[0] + 9], layers=1)
+    n_pages = (9 << 29) // c.stride
+    big = [torch.empty((n_pages, c.stride), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    for b, x in zip(big, c.dev):
+        b[n_pages - c.n_pages:] = x
+    far = np.where(tables >= 0, tables + (n_pages - c.n_pages), -1)
+    paged = PagedCache(1, n_pages, c.stride, DEV, [big[0]], [big[1]])
+    lens = up(np.zeros(1))
+    batch = T.make_batch(1, new[0], up(np.array([0, new[0]])), up(np.array([new[0] + 9])), up(far), far.shape[2])
+    T.tl_keep(c.ctx, torch.cuda.current_stream(), batch, paged.tl(), up(np.array([len(kept[0])])), up(np.array(kept[0] + [0] * (new[0] - len(kept[0])))), lens)
+    torch.cuda.synchronize()
+    want = hc.keep(c, tables, new, [new[0] + 9], kept)
+    c.dev = torch.stack([b[n_pages - c.n_pages:] for b in big])
+    c.same()
+    assert lens.tolist() == want[0]

@@ -209,3 +209,54 @@ def test_captured():
         equal(out, t, "tables")
         equal(d_refs, refs, "counts")
         c.same("replay %d" % seed)
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond the first 4 GiB of a cache, copied and branched."""
+    from paper_2609_39358_amd.device import PagedCache
+
+    c = Pages(8, 16, 8, 128, "fp8_scaled", 12, 1).up()
+    n_pages = (9 << 29) // c.stride
+    far = n_pages - c.n_pages
+    big = [torch.empty((n_pages, c.stride), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    for b, x in zip(big, c.dev):
+        b[far:] = x
+    paged = PagedCache(1, n_pages, c.stride, DEV, [big[0]], [big[1]])
+    src, dst, rows = np.array([[0, 5]]), np.array([[9, 2]]), np.array([16, 7])
+    T.tl_pages_copy(c.ctx, stream(), paged.tl(), 2, up(src + far), up(dst + far), up(rows))
+    hc.copy(c, src, dst, rows)
+    refs = np.ones((1, n_pages), np.int32)
+    refs[0, far + 10] = 0
+    tables = np.array([[[far + 1, far + 4, -1]]])
+    size = T.tl_pages_workspace_bytes(c.ctx, 1, n_pages)
+    out, lens = torch.zeros((1, 1, 3), dtype=torch.int32, device=DEV), up(np.zeros(1))
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    d_refs = up(refs)
+    T.tl_pages_fork(c.ctx, stream(), T.make_pool(d_refs), paged.tl(), 1, up(np.array([27])), up(tables), 1, up(np.zeros(1)), lens, out, 3, ws, size)
+    hc.copy(c, np.array([[4]]), np.array([[10]]), [11])
+    torch.cuda.synchronize()
+    assert out.tolist() == [[[far + 1, far + 10, -1]]] and lens.tolist() == [27]
+    assert d_refs[0, far + 1].item() == 2 and d_refs[0, far + 10].item() == 1
+    c.dev = torch.stack([b[far:] for b in big])
+    c.same()
+
+
+def test_copies_captured():
+    c = Pages(9, 16, 4, 64, "bf16", 40, 3).up()
+    src, dst, rows = (up(np.zeros((1, 6))) for _ in range(3))
+    cache = c.paged.tl()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        T.tl_pages_copy(c.ctx, side, cache, 6, src, dst, rows)
+    for turn in range(3):
+        ids = c.r.permutation(40)[:12]
+        n = c.r.integers(0, 17, 6)
+        for x, y in ((src, ids[:6]), (dst, ids[6:]), (rows, n)):
+            x.copy_(up(y[None]))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        hc.copy(c, ids[None, :6], ids[None, 6:], n)
+        c.same("replay %d" % turn)

@@ -101,6 +101,7 @@ def test_free(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(n_keep=None), T.TL_EINVAL), (dict(rows=None), T.TL_EINVAL), (dict(rows=TABLES + 1), T.TL_EINVAL), (dict(len_out=None), T.TL_EINVAL),
     (dict(len_out=FAKE), T.TL_EINVAL), (dict(len_out=PARENT), T.TL_EINVAL), (dict(b=batch(d_row_off=None)), T.TL_EINVAL),
+    (dict(len_out=TABLES + 4), T.TL_EINVAL), (dict(b=batch(d_row_off=OUT - 4)), T.TL_EINVAL),
     (dict(b=batch(n_rows=0, d_kv_len=None)), T.TL_EINVAL), (dict(b=batch(d_tables=None)), T.TL_EINVAL), (dict(b=batch(n_rows=1 << 24)), T.TL_ERANGE),
     (dict(b=batch(n_reqs=1 << 20)), T.TL_ERANGE), (dict(b=batch(n_reqs=0, d_row_off=None), n_keep=None), T.TL_OK)])
 def test_keep(kw, status):
