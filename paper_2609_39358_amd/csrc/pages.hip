@@ -508,14 +508,14 @@ __device__ __forceinline__ void say_kept(const KeepArgs& a, const Kept& k, uint3
 // Few rows: a wavefront by itself takes L 16-byte columns (scaled pages: a head) of one
 // request's rows in some slabs, one after another, and waits for no other. What it costs is
 // instructions and one wait after another, not bytes: so a step's places are found once for
-// all its slabs, a step has as many rows as the lanes hold (accepted drafts are few), and
-// registers are few, for many wavefronts on a SIMD. 96 requests that keep up to 7 of up to 48
-// rows, 32 layers of 8 heads of 128 in 8 bits: 26 us; with 32 rows a step and the next slab's
-// asked for ahead 50 (186 registers and more), a workgroup for all heads and a slab 53. (With
-// 20 of 64 rows kept 125, 85 and - : two steps for each page.)
-template <int L>
+// all its slabs, a step has as many rows as the lanes hold once (accepted drafts are few; twice
+// where requests bring many rows), and registers are few, for many wavefronts on a SIMD. 96
+// requests that keep up to 7 of up to 48 rows, 32 layers of 8 heads of 128 in 8 bits: 23 us; with
+// 32 rows a step and the next slab's asked for ahead 50 (186 registers and more), a workgroup for
+// all heads and a slab 53.
+template <int L, int U>
 struct FewRows {
-  static constexpr uint32_t R = 64 / L, U = L == 16 ? 2 : 1, N = R * U;  // rows at a time, times, rows of a step
+  static constexpr uint32_t R = 64 / L, N = R * U;  // rows at a time, rows of a step
 };
 
 __device__ __forceinline__ int64_t shuffled(int64_t x, uint32_t lane) {
@@ -524,15 +524,15 @@ __device__ __forceinline__ int64_t shuffled(int64_t x, uint32_t lane) {
 }
 
 // Rows that have been asked for are there, before anything is written after this.
-template <uint32_t U>
+template <int U>
 __device__ __forceinline__ void arrived(u32x4 (&x)[U]) {
 #pragma unroll
-  for (uint32_t u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]) : : "memory");
+  for (int u = 0; u < U; ++u) asm volatile("" : "+v"(x[u]) : : "memory");
 }
 
-template <bool FP8, int L>
+template <bool FP8, int L, int U>
 __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t slab1, uint32_t block) {
-  typedef FewRows<L> F;
+  typedef FewRows<L, U> F;
   const uint32_t lane = threadIdx.x & 63, j = lane % L, sub = lane / L, column = block * L + j;
   const bool there = column < a.columns;
   const Kept k = kept_of(a, r);
@@ -548,15 +548,15 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
     const bool whole = ask <= F::N;  // they are held, not read again
     const uint32_t last = a.b.page.div(pos + ask - 1);
     // this lane's rows
-    int64_t from[F::U], to[F::U], from_scale[F::U], to_scale[F::U];
-    uint32_t page[F::U];
+    int64_t from[U], to[U], from_scale[U], to_scale[U];
+    uint32_t page[U];
     auto find = [&](uint32_t i, uint32_t count) {
       RowMove m = {0, 0, 0, 0, 0};
       const bool fine = lane >= count || move_of(a, k, i + lane, own, m);
       const uint64_t none = ~__ballot(fine);
       const int64_t f = m.from_page + (int64_t)m.from_row * a.c.row_bytes, t = m.to_page + (int64_t)m.to_row * a.c.row_bytes;
 #pragma unroll
-      for (uint32_t u = 0; u < F::U; ++u) {
+      for (int u = 0; u < U; ++u) {
         const uint32_t at = u * F::R + sub;
         from[u] = shuffled(f, at) + column * 16;
         to[u] = shuffled(t, at) + column * 16;
@@ -576,8 +576,8 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
       if (!ask) break;
       if constexpr (FP8) first_scale_at = shuffled(to_scale[0], 0);
     }
-    u32x4 x[F::U] = {};
-    uint32_t scale[F::U] = {};
+    u32x4 x[U] = {};
+    uint32_t scale[U] = {};
 #pragma unroll 1
     for (uint32_t slab = slab0; slab < slab1; ++slab) {
       const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)bases, slab - slab0);
@@ -585,7 +585,7 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
       const Bytes base = (Bytes)((uint64_t)hi << 32 | lo);
       auto load = [&](uint32_t count) {
 #pragma unroll
-        for (uint32_t u = 0; u < F::U; ++u)
+        for (int u = 0; u < U; ++u)
           if (u * F::R + sub < count && there) {
             x[u] = *(Granules)(base + from[u]);
             if constexpr (FP8) scale[u] = base[from_scale[u]];
@@ -595,15 +595,15 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
         load(ask);
         arrived(x);
 #pragma unroll
-        for (uint32_t u = 0; u < F::U; ++u)
+        for (int u = 0; u < U; ++u)
           if (u * F::R + sub < ask && there) *(Granules)(base + to[u]) = x[u];
       } else {
-        uint32_t needs[F::U], first = kScaleMin, old = 0;  // scale bytes of a row's new page, and of the step's first one
+        uint32_t needs[U], first = kScaleMin, old = 0;  // scale bytes of a row's new page, and of the step's first one
         // what the pages of the rows that were read need
         auto needs_of = [&](uint32_t count) {
-          uint32_t mine[F::U];
+          uint32_t mine[U];
 #pragma unroll
-          for (uint32_t u = 0; u < F::U; ++u) {
+          for (int u = 0; u < U; ++u) {
             scale[u] = scale_held(scale[u]);
             float m = u * F::R + sub < count && there ? largest_code(x[u]) : 0.f;
 #pragma unroll
@@ -614,13 +614,13 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
           for (uint32_t p = page0; p <= last; ++p) {  // two pages, mostly
             uint32_t m = kScaleMin;
 #pragma unroll
-            for (uint32_t u = 0; u < F::U; ++u)
+            for (int u = 0; u < U; ++u)
               if (u * F::R + sub < count && page[u] == p) m = max(m, mine[u]);
 #pragma unroll
             for (int d = L; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
             if (p == page0) first = max(first, m);
 #pragma unroll
-            for (uint32_t u = 0; u < F::U; ++u)
+            for (int u = 0; u < U; ++u)
               if (page[u] == p) needs[u] = m;
           }
         };
@@ -658,7 +658,7 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
         auto store = [&](uint32_t count) {
           arrived(x);
 #pragma unroll
-          for (uint32_t u = 0; u < F::U; ++u) {
+          for (int u = 0; u < U; ++u) {
             if (u * F::R + sub >= count || !there) continue;
             const uint32_t now = page[u] == page0 ? first : needs[u];
             *(Granules)(base + to[u]) = scale[u] == now ? x[u] : rescale(x[u], scale[u], now);
@@ -672,7 +672,7 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
             const uint32_t count = find(done + i, min(F::N, ask - i));
             load(count);
 #pragma unroll
-            for (uint32_t u = 0; u < F::U; ++u) scale[u] = scale_held(scale[u]);
+            for (int u = 0; u < U; ++u) scale[u] = scale_held(scale[u]);
             store(count);
           }
           if (there && j == 0 && sub == 0) base[first_scale_at] = (uint8_t)first;  // no row asks for the one before any more
@@ -684,18 +684,19 @@ __device__ void keep_few(const KeepArgs& a, uint32_t r, uint32_t slab0, uint32_t
   if (slab0 == 0 && block == 0 && lane == 0) say_kept(a, k, r, done, bad);
 }
 
-template <bool FP8, int L>
+template <bool FP8, int L, int U>
 __global__ __launch_bounds__(kThreads) void k_keep_few(KeepArgs a) {
   const uint64_t per = (uint64_t)((a.c.n_slabs + a.slabs - 1) / a.slabs) * a.blocks, items = a.b.n_reqs * per;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   for (uint64_t item = (uint64_t)blockIdx.x * (kThreads / 64) + wave; item < items; item += (uint64_t)gridDim.x * (kThreads / 64)) {
     const uint32_t rest = (uint32_t)(item % per), slab0 = rest / a.blocks * a.slabs;
-    keep_few<FP8, L>(a, (uint32_t)(item / per), slab0, min(slab0 + a.slabs, a.c.n_slabs), rest % a.blocks);
+    keep_few<FP8, L, U>(a, (uint32_t)(item / per), slab0, min(slab0 + a.slabs, a.c.n_slabs), rest % a.blocks);
   }
 }
 
-// Many rows: bounded by memory. A workgroup takes C 16-byte columns of a slab, kRows rows
-// at a time with U more behind each.
+// Many rows: a workgroup takes C 16-byte columns of a slab, R rows at a time with U more
+// behind each. In bf16 bounded by memory; with scales by what a step waits for, one thing
+// after another.
 template <bool FP8, int C, int U>
 struct KeepLds {
   static constexpr uint32_t R = kThreads / C, N = R * U;  // rows at a time, rows of a step
@@ -1000,12 +1001,25 @@ int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const ui
     TimedLaunch timed(TL_KERNEL_KEEP, stream);
     const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED;
     if (many) {
-      a.blocks = (a.columns + 15) / 16;
-      const dim3 grid(grid_of((uint64_t)batch->n_reqs * a.c.n_slabs * a.blocks));
-      if (fp8)
+      // Columns of a workgroup and rows of a thread: small workgroups' worth of columns, and many
+      // rows, where there are few workgroups. us with 16 and 8 / 8 and 4 / 8 and 8 columns and rows: in
+      // 8 bits, 16 heads of 128, 8,003 rows of one request in 24 slabs 779 / 482 / 454, 1,443 in 4 slabs of
+      // 256-token pages 121 / 71 / 52, 1,500 of each of 8 requests 540 / 440 / 548; in bf16 362 / 343 / 339,
+      // 31 / 24 / 19, 494 / 531 / 533.
+      const uint64_t rows = (uint64_t)batch->n_reqs * a.c.n_slabs, small = rows * ((a.columns + 7) / 8);
+      const bool wide = fp8 ? ctx->D == 256 : small >= 2048;
+      a.blocks = wide ? (a.columns + 15) / 16 : (a.columns + 7) / 8;
+      const dim3 grid(grid_of(rows * a.blocks));
+      if (fp8 && wide)
         hipLaunchKernelGGL((k_keep<true, 16, 8>), grid, dim3(kThreads), 0, s, a);
-      else
+      else if (fp8 && small >= 1024)
+        hipLaunchKernelGGL((k_keep<true, 8, 4>), grid, dim3(kThreads), 0, s, a);
+      else if (fp8)
+        hipLaunchKernelGGL((k_keep<true, 8, 8>), grid, dim3(kThreads), 0, s, a);
+      else if (wide)
         hipLaunchKernelGGL((k_keep<false, 16, 8>), grid, dim3(kThreads), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_keep<false, 8, 8>), grid, dim3(kThreads), 0, s, a);
     } else {
       const uint32_t L = fp8 ? ctx->D / 16 : 8;
       a.blocks = (a.columns + L - 1) / L;
@@ -1016,14 +1030,22 @@ int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const ui
       a.slabs = a.c.n_groups == 1 ? (uint32_t)std::clamp<uint64_t>(all / 6144 & ~1ull, 2, 8) : 2;
       const uint64_t items = (uint64_t)batch->n_reqs * ((a.c.n_slabs + a.slabs - 1) / a.slabs) * a.blocks;
       const dim3 grid(grid_of((items + kThreads / 64 - 1) / (kThreads / 64)));
+      // Rows of a step: once or twice what the lanes hold. us, 96 requests of 48 rows that keep 7 / 12
+      // / 20 of them, heads of 128 in 8 bits 23 / 63 / 73 with 8 rows, 36 / 41 / 54 with 16; heads of 256 46 / 110
+      // and 73 / 87; in bf16 35 / 58 and 35 / 48. Up to 64 rows most are drafts that were refused.
+      const bool more = batch->n_rows / batch->n_reqs > 64;
       if (!fp8)
-        hipLaunchKernelGGL((k_keep_few<false, 8>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_keep_few<false, 8, 2>), grid, dim3(kThreads), 0, s, a);
       else if (L == 4)
-        hipLaunchKernelGGL((k_keep_few<true, 4>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_keep_few<true, 4, 1>), grid, dim3(kThreads), 0, s, a);
+      else if (L == 8 && more)
+        hipLaunchKernelGGL((k_keep_few<true, 8, 2>), grid, dim3(kThreads), 0, s, a);
       else if (L == 8)
-        hipLaunchKernelGGL((k_keep_few<true, 8>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_keep_few<true, 8, 1>), grid, dim3(kThreads), 0, s, a);
+      else if (more)
+        hipLaunchKernelGGL((k_keep_few<true, 16, 4>), grid, dim3(kThreads), 0, s, a);
       else
-        hipLaunchKernelGGL((k_keep_few<true, 16>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((k_keep_few<true, 16, 2>), grid, dim3(kThreads), 0, s, a);
     }
   }
   return launched();

@@ -96,6 +96,23 @@ def test_many_rows(cache, P, H, D, layers, group_of, pad):
     assert lens == want[0] and status == want[1] and set(status) == {T.ACCEPT}
 
 
+@pytest.mark.parametrize("cache,H,D,new,layers", [("fp8_scaled", 4, 128, 90, 2), ("fp8_scaled", 2, 256, 90, 2), ("fp8_scaled", 6, 64, 90, 2), ("bf16", 4, 128, 90, 2),
+                                                  ("fp8_scaled", 16, 128, 300, 17), ("bf16", 16, 64, 300, 33), ("fp8_scaled", 3, 64, 300, 1),
+                                                  ("fp8_scaled", 3, 256, 300, 1), ("bf16", 3, 128, 300, 1)])
+@pytest.mark.parametrize("P", [16, 104])
+def test_both_sides_of_the_rules(cache, H, D, new, layers, P):
+    """Requests of some and of many rows, few and many workgroups, pages of fewer and more rows than a step."""
+    if cache == "bf16" and P * H * D % 512:
+        pytest.skip("slabs are whole KiB")
+    r = np.random.default_rng(15)
+    news = [new, new + 17, new + 40, new]
+    kv_len = [a + int(h) for a, h in zip(news, r.integers(0, 40, 4))]
+    kept = [some(r, news[0], 40), list(range(news[1] // 2, news[1])), some(r, news[2], 9), [0, 1] + list(range(30, news[3], 2))]
+    c, tables = make(16, P, H, D, cache, news, kv_len, layers=layers)
+    lens, status, want = run(c, tables, news, kv_len, kept)
+    assert lens == want[0] and status == want[1] and set(status) == {T.ACCEPT}
+
+
 @pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
 @pytest.mark.parametrize("P", [16, 104])
 @pytest.mark.parametrize("more", [1, 10])
