@@ -40,8 +40,8 @@ def build(verbose: bool = False, extra_hip_flags=(), out: str = OUT, build_dir: 
     cxx = os.environ.get("CXX") or shutil.which("g++") or "g++"
     os.makedirs(build_dir, exist_ok=True)
     inc = ["-I", INCLUDE, "-I", CSRC]
-    sources = ("ctx.cpp", "sha256.cpp", "file_io.cpp", "operators.cpp", "kernels.hip", "chain.hip", "append.hip", "attend.hip",
-               "attend_tree.hip", "pages.hip")
+    sources = ("attend_tree.hip", "attend.hip", "pages.hip", "append.hip", "chain.hip", "kernels.hip",  # the longest first
+               "ctx.cpp", "sha256.cpp", "file_io.cpp", "operators.cpp")
     obj = lambda src: os.path.join(build_dir, src + ".o")  # noqa: E731
 
     def compile_one(src):

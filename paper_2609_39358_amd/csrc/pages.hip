@@ -1001,11 +1001,12 @@ int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const ui
     TimedLaunch timed(TL_KERNEL_KEEP, stream);
     const bool fp8 = ctx->dtype == TL_DTYPE_FP8_SCALED;
     if (many) {
-      // Columns of a workgroup and rows of a thread: small workgroups' worth of columns, and many
-      // rows, where there are few workgroups. us with 16 and 8 / 8 and 4 / 8 and 8 columns and rows: in
-      // 8 bits, 16 heads of 128, 8,003 rows of one request in 24 slabs 779 / 482 / 454, 1,443 in 4 slabs of
-      // 256-token pages 121 / 71 / 52, 1,500 of each of 8 requests 540 / 440 / 548; in bf16 362 / 343 / 339,
-      // 31 / 24 / 19, 494 / 531 / 533.
+      // Columns of a workgroup (a head's at least) and rows of a thread. Few columns make more
+      // workgroups and longer steps; short steps make room for more workgroups at a time. us with
+      // 16 columns and 8 rows / 8 and 4 / 8 and 8: in 8 bits, 16 heads of 128, 8,003 rows of one
+      // request in 24 slabs 779 / 482 / 454, 1,443 in 4 slabs of 256-token pages 121 / 71 / 52, 1,500
+      // of each of 8 requests in 24 slabs 540 / 440 / 548; the same in bf16 362 / 343 / 339, 31 / 24 / 19,
+      // 494 / 531 / 533.
       const uint64_t rows = (uint64_t)batch->n_reqs * a.c.n_slabs, small = rows * ((a.columns + 7) / 8);
       const bool wide = fp8 ? ctx->D == 256 : small >= 2048;
       a.blocks = wide ? (a.columns + 15) / 16 : (a.columns + 7) / 8;
