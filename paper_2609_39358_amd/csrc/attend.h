@@ -66,6 +66,7 @@ struct AttendArgs {
   const uint64_t* tree;      // [rows][tree_words] which of its request's new tokens a row sees, of a tree
   const int32_t* tree_pos;   // [rows] positions, where there is a window
   uint32_t tree_words;
+  uint32_t tree_whole;       // no tile is cut: a unit is a tile
 };
 
 namespace {
@@ -136,11 +137,18 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Request& q, u
   return s;
 }
 
+// Units of a tile.
+template <int MODE>
+__device__ __forceinline__ uint32_t units_of_tile(const AttendArgs& a, const Request& q, uint32_t tile) {
+  if (MODE == kTree && a.tree_whole) return 1;
+  return q.cost + q.weight * span_of<MODE>(a, q, tile).n;
+}
+
 // Units of a request's tiles tile0, tile0 + step, ...
 template <int MODE>
 __device__ __forceinline__ uint64_t units_of(const AttendArgs& a, const Request& q, uint32_t tile0, uint32_t step) {
   uint64_t n = 0;
-  for (uint32_t t = tile0; t < q.tiles; t += step) n += q.cost + q.weight * span_of<MODE>(a, q, t).n;
+  for (uint32_t t = tile0; t < q.tiles; t += step) n += units_of_tile<MODE>(a, q, t);
   return n;
 }
 
@@ -225,7 +233,7 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
       c.first += c.head * units;
       c.tile = 0;
       for (;;) {
-        const uint32_t k = q.cost + q.weight * span_of<MODE>(a, q, c.tile).n;
+        const uint32_t k = units_of_tile<MODE>(a, q, c.tile);
         if (c.at < c.first + k) return true;
         c.first += k;
         ++c.tile;
@@ -239,7 +247,13 @@ __device__ bool plan(const AttendArgs& a, PlanLds& l, Cursor& c) {
 
 // The blocks [k0, k1) of the cursor's tile that begin in its run (none where the run
 // ends within the tile's cost, or begins within its last block), and the tile's end.
-__device__ __forceinline__ uint64_t blocks_of(const Cursor& c, const Request& q, const Span& s, uint32_t& k0, uint32_t& k1) {
+template <int MODE>
+__device__ __forceinline__ uint64_t blocks_of(const AttendArgs& a, const Cursor& c, const Request& q, const Span& s, uint32_t& k0, uint32_t& k1) {
+  if (MODE == kTree && a.tree_whole) {
+    k0 = 0;
+    k1 = s.n;
+    return c.first + 1;
+  }
   const int64_t n = (int64_t)s.n * q.weight;
   const uint64_t block0 = c.first + q.cost;
   const uint32_t u0 = (uint32_t)min(n, max((int64_t)0, (int64_t)(c.at - block0)));
@@ -798,7 +812,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a
   for (bool first = true; cur.at < cur.end; first = false) {
     const Span s = span_of<MODE>(a, q, cur.tile);
     uint32_t k0, k1;
-    const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
+    const uint64_t tile_end = blocks_of<MODE>(a, cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
     if (k0 < k1) segment16<D, FP8, EVEN, 4, MODE>(a, l.s, cur, q, s, k0, k1);
     cur.at = min(cur.end, tile_end);
@@ -1318,7 +1332,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_attend_many(AttendArgs a) {
   for (bool first = true; cur.at < cur.end; first = false) {
     const Span s = span_of<MODE>(a, q, cur.tile);
     uint32_t k0, k1;
-    const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
+    const uint64_t tile_end = blocks_of<MODE>(a, cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
     if (k0 == k1) {
       // none

@@ -368,7 +368,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void k_attend_rows(AttendArgs a)
   for (bool first = true; cur.at < cur.end; first = false) {
     const Span s = span_of<kTree>(a, q, cur.tile);
     uint32_t k0, k1;
-    const uint64_t tile_end = blocks_of(cur, q, s, k0, k1);
+    const uint64_t tile_end = blocks_of<kTree>(a, cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
     if (k0 < k1) segment_rows<D, FP8, EVEN>(a, l.s, cur, q, s, k0, k1);
     cur.at = min(cur.end, tile_end);
@@ -417,6 +417,20 @@ Shape rows_shape(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_
   return s;
 }
 
+// Whether each tile goes to one workgroup as a whole. Where a layer has a window, tiles have
+// about as many keys (the window's and the new ones), and if they fill the workgroups, in some
+// rounds, to a good part, there is little to even out: no tile is started and ended twice, no parts are written,
+// and there is no join. us, cut / whole, window of 1,024, 16 heads of 128, bf16, requests of 77 tokens (16
+// tiles each, 256 workgroups): 8 requests 75 / 68, 10 81 / 69, 12 93 / 73, 16 101 / 77, 17 108 / 133, 24 142 / 135, 32
+// 172 / 143; of 30 tokens (512 workgroups) 32 requests 102 / 82, 44 166 / 156, 60 246 / 213; of 12
+// (k_attend_rows, 4 tiles each) 44 104 / 88, 64 138 / 119, 110 220 / 201; 16 of 1 to 77 tokens 96 / 100. (Without a
+// window the lengths, which only the device has, may differ by any factor.)
+bool whole_tiles(const tl_ctx* ctx, uint32_t layer, const Shape& s, const Kind& k, uint64_t n_reqs, uint64_t n_rows) {
+  const uint64_t tokens = (n_rows + n_reqs - 1) / n_reqs, tiles = n_reqs * k.heads * ((tokens + k.tile_rows - 1) / k.tile_rows);
+  const uint64_t rounds = (tiles + s.workers - 1) / s.workers;
+  return ctx->window[layer] && tiles * 5 >= rounds * s.workers * 3;
+}
+
 }  // namespace
 
 size_t attend_tree_needs(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_t n_rows) {
@@ -436,6 +450,7 @@ int launch_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl
   const bool rows = by_rows(ctx, n_q_heads, batch->n_reqs, batch->n_rows);
   const Shape sh = rows ? rows_shape(ctx, n_q_heads, batch->n_reqs, batch->n_rows) : shape_of(ctx, n_q_heads, batch->n_reqs, batch->n_rows);
   fill(a, sh, ctx, layer, batch, n_q_heads, q, cache, scale, out, d_lse, d_ws);
+  if (whole_tiles(ctx, layer, sh, rows ? sh.kind[0] : sh.kind[1], batch->n_reqs, batch->n_rows)) a.tree_whole = a.least = 1;
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();
   by_cache(ctx, [&](auto D, auto fp8, auto even) {
@@ -446,7 +461,7 @@ int launch_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl
       else
         launch_many<D(), fp8(), even(), kTree>(sh, s, a);
     }
-    launch_join<D()>(sh, s, a);
+    if (!a.tree_whole) launch_join<D()>(sh, s, a);
   });
   return hipGetLastError() == hipSuccess ? TL_OK : TL_EDEVICE;
 }

@@ -153,6 +153,19 @@ def test_windows(cache, name, P, H, D, Hq, window):
 
 
 @pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("H,D,Hq,n,new", [(16, 64, 16, 40, 3), (16, 64, 32, 90, 5), (6, 128, 6, 60, 2), (16, 64, 16, 21, 70), (16, 128, 32, 10, 71), (16, 128, 32, 17, 66),
+                                          (16, 256, 16, 10, 20), (1, 256, 4, 170, 6)])
+def test_windows_of_many_requests(cache, ragged, H, D, Hq, n, new):
+    """As many tiles as workgroups, or some times as many: on each kernel."""
+    r = np.random.default_rng(17)
+    news = [int(x) for x in r.integers(0, 2 * new, n)] if ragged else [new] * n
+    c = Paged(18, 16, H, D, cache, news, [a + int(b) for a, b in zip(news, r.integers(0, 120, n))], window=50).fill(spread=1).up()
+    see, depth = trees(c, r, 3)
+    check(c, Hq, see, depth, -(-max(news) // 64))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8_scaled"])
 @pytest.mark.parametrize("name", list(BATCHES))
 @pytest.mark.parametrize("P,H,D,Hq", [(16, 2, 128, 8), (104, 1, 64, 8), (32, 2, 256, 4)])
 def test_any_masks(cache, name, P, H, D, Hq):
