@@ -631,20 +631,29 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     // window takes four, one after another.
     if (a.step == 1 && a.b.n_rows > (1u << 22)) a.step = 4;
     a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
-    // Workgroups that fill the device. Fewer windows give their heads to several (128 windows
-    // of 16 rows, 16 heads: 36 us with one, 19 with four each; 512: 41 and 49), and long ones
-    // are cut more readily (96 windows of 256 rows: 558 and 216).
-    const uint32_t many = a.step > 64 ? 1024 : 512;
-    a.splits = a.step > 1 && a.n_windows < many ? std::min((many + a.n_windows - 1) / a.n_windows, (ctx->H + kWaves - 1) / kWaves) : 1;
-    a.split_heads = (ctx->H + a.splits - 1) / a.splits;
-    a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
     // Fragments that begin in one window are written one after another, so few windows are made
-    // shorter. us before and after, 8 heads of 128 on pages of 16 rows: 96 requests of 24 rows 22 and
-    // 18 (with norms 36 and 25), 16 of up to 24 rows 16 and 10; 384 windows would take 47 for 40.
-    while (a.step > 2 && a.n_windows < 256) {
+    // shorter, but not much shorter than long fragments, as each of them takes a place to find that it
+    // is empty. us with two rows a window at least / 64 where fragments are longer: one request of 3,000
+    // tokens on pages of 256, 16 heads of 128, 214 / 36, 24 of 300 226 / 73. 96 requests of 24 rows on pages
+    // of 16 take 18 with shorter windows and 22 without.
+    const uint32_t rows = a.step, R = 64 / (ctx->D / 16);
+    while (a.step > (rows > 64 ? 64 : 2) && a.n_windows < 256) {
       a.step = (a.step + 1) / 2;
       a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
     }
+    // A window's heads go to several workgroups, up to about 1,100 in all (half of which have no
+    // fragment): each to so many heads as its wavefronts take at once, not one round after another (put_fragment).
+    // us with four heads each, up to 512 workgroups / with this: 12 requests of up to 24 rows, 8 heads of 128 on pages of
+    // 16, with norms 14 / 11, 40 15 / 12, 96 21 / 21; 3 of 16 rows, 16 heads 9.4 / 7.5; 24,573 tokens on pages of 256
+    // 410 / 345 (up to 2,200 workgroups 410).
+    const uint32_t held = a.step <= R || (a.n_windows >= 256 && a.step <= kWaves * R) ? 1 : 2;
+    uint32_t span = 1, share = 1;
+    while (span < rows && span < R) span *= 2;
+    while (share < kWaves && held * span * share < rows) share *= 2;
+    const uint32_t at_once = kWaves / share * (R / span);
+    a.splits = std::max(1u, std::min(1100 / a.n_windows, (ctx->H + at_once - 1) / at_once));
+    a.split_heads = std::min(ctx->H, ((ctx->H + a.splits - 1) / a.splits + at_once - 1) / at_once * at_once);
+    a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
   }
   const uint32_t single = !fp8 || q || d_status ? (a.b.n_rows + kWaves - 1) / kWaves : 0;
   const uint32_t grid = a.n_windows * a.splits + single;
