@@ -1,5 +1,7 @@
 // tl_append, tl_append_norm: the new tokens' keys and values into the pages of a cache,
 // keys and queries normed and rotated on the way.
+#include <float.h>
+
 #include <algorithm>
 
 #include "paged.h"
@@ -178,11 +180,13 @@ __device__ __forceinline__ void norm(const AppendArgs& a, float* x) {
   float eps = a.eps;
   if (!(s < __uint_as_float(kInfinite))) {
     // Values of 2^60 and more: their squares pass 32 bits, but not those of 2^-70 times
-    // them (and values that are not finite stay what they are).
+    // them (and values that are not finite stay what they are). eps is lost beside these
+    // squares, unless all of them are 0: equal values less their mean, which the smallest
+    // normal number in its place leaves 0.
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = x[i] * 0x1p-70f;
     s = centered_squares<D>(a.center, y);
-    eps = 0.f;
+    eps = FLT_MIN;
   }
   const float r = 1.f / __builtin_sqrtf(s + eps);
 #pragma unroll
