@@ -792,7 +792,8 @@ def _check_pool(ctx: Ctx, pool: tl_pool):
 def _words(x, n: int, what: str):
     if x is None:
         return None
-    if getattr(x, "dtype", None) is _I32 and x.is_cuda and x.is_contiguous() and x.numel() >= n:
+    dtype = getattr(x, "dtype", None)  # (an address has none, and _I32 is None without torch)
+    if dtype is not None and dtype is _I32 and x.is_cuda and x.is_contiguous() and x.numel() >= n:
         return x.data_ptr()  # (these calls are small: their checks are what they cost)
     _of_type(x, _WORDS, what)
     _fits(x, 4 * n, what)
