@@ -630,7 +630,13 @@ int tl_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_bat
  * A pool counts how many table rows name each page; a page that none names is free.
  * Counts start as the caller sets them (0 for free pages; a page that must never be
  * given out: 1). Counts of 0 and less are free. Which pages a call gives depends on
- * the counts and the requests' order alone: the lowest free ones. */
+ * the counts and the requests' order alone: of each group's free pages, lowest first,
+ * every request is meant to have the next ones, as many as it wants there. A request
+ * whose pages are not all there, in some group, is refused (TL_MISSING): it takes
+ * nothing, but no later request of the call is given what was meant for it, in any group.
+ * So none overtakes it: once a group's pages have run out, all later requests that want
+ * pages of it are refused too, also if they want fewer than are left. To serve those
+ * all the same, call again without the refused one, or name large requests last. */
 typedef struct tl_pool {
   int32_t* d_refs; /* device [n_groups][n_pages] */
   int64_t n_pages; /* as in tl_cache */
@@ -652,8 +658,8 @@ int tl_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, size_t
  * not overlapping d_tables) names these and -1 behind them; d_len_out[i] is its length.
  * Entries of the parent's that name no page stay -1. d_status (device [n] or NULL):
  * TL_ACCEPT; TL_BADARG for a parent outside [0, n_parents) or longer than its row;
- * TL_MISSING where the pool has no page left for it, as branches are served in order
- * (both: a row of -1, length 0, nothing is counted). Two kernels. */
+ * TL_MISSING where the pool has no page for it, as tl_pool says (both: a row of -1,
+ * length 0, nothing is counted). Two kernels. */
 int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl_cache* cache, size_t n_parents,
                   const uint32_t* d_kv_len, const int32_t* d_tables, size_t n, const int32_t* d_parent,
                   uint32_t* d_len_out, int32_t* d_tables_out, size_t table_width, uint8_t* d_status,
@@ -662,8 +668,8 @@ int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl
 /* Pages for more tokens: each of the entries of request i's table row between
  * d_have[i] and d_want[i] tokens (the pages that begin there) that names no page gets a
  * free one, in every group. d_status (device [n] or NULL): TL_ACCEPT; TL_BADARG where
- * d_want is past the table row; TL_MISSING where what is left does not suffice, as
- * requests are served in order (both: nothing is taken for it). One kernel. */
+ * d_want is past the table row (it counts as wanting none); TL_MISSING where the pool
+ * has no pages for it, as tl_pool says (both: nothing is taken for it). One kernel. */
 int tl_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, const uint32_t* d_have,
                   const uint32_t* d_want, int32_t* d_tables, size_t table_width, uint8_t* d_status,
                   void* d_workspace, size_t workspace_bytes);

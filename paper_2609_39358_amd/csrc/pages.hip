@@ -74,10 +74,11 @@ __global__ __launch_bounds__(kThreads) void k_pages_copy(CopyArgs a) {
 }
 
 // ---- whose pages are whose ---------------------------------------------------------
-// A pool counts each page's owners; one that has none is free. Requests are given
-// the lowest free pages, in their order: which ones does not depend on when a
-// kernel's threads run. Counts change by atomic additions, whose order does not
-// matter to their sum.
+// A pool counts each page's owners; one that has none is free. Of the lowest free
+// pages each request is meant to have those behind what the requests before it want,
+// whether they are served or not: a prefix sum, which does not depend on when a
+// kernel's threads run, and by which none overtakes one that has to be refused.
+// Counts change by atomic additions, whose order does not matter to their sum.
 struct PoolArgs {
   int32_t* refs;  // [n_groups][n_pages]
   uint32_t n_pages, n_groups, page_tokens;

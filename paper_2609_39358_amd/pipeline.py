@@ -438,7 +438,8 @@ class PagePool:
     host step in between. `refs` i32 [n_groups, n_pages] counts each page's owners;
     `used` lists pages that are never given out. Tables are i32 [n_groups, n, width]
     with -1 where a request has no page; `status` has the verdicts of the last take()
-    or fork() (valid after the stream syncs)."""
+    or fork() (valid after the stream syncs). Requests are served in order and none overtakes
+    one that is refused for want of pages (tl_pool): name large ones last."""
 
     def __init__(self, ctx: T.Ctx, cache: PagedCache, used=(), stream=None):
         self.ctx, self.cache, self._pages = ctx, cache.tl(), cache
