@@ -666,8 +666,8 @@ int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl
                   void* d_workspace, size_t workspace_bytes);
 
 /* Pages for more tokens: each of the entries of request i's table row between
- * d_have[i] and d_want[i] tokens (the pages that begin there) that names no page gets a
- * free one, in every group. d_status (device [n] or NULL): TL_ACCEPT; TL_BADARG where
+ * d_have[i] and d_want[i] tokens (the pages that begin there) that names no page (an id
+ * outside [0, n_pages)) gets a free one, in every group. d_status (device [n] or NULL): TL_ACCEPT; TL_BADARG where
  * d_want is past the table row (it counts as wanting none); TL_MISSING where the pool
  * has no pages for it, as tl_pool says (both: nothing is taken for it). One kernel. */
 int tl_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n, const uint32_t* d_have,

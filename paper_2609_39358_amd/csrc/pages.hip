@@ -123,6 +123,9 @@ __device__ __forceinline__ uint32_t last_page(const PoolArgs& a, const Fork& f, 
   return (uint32_t)a.tables[((uint64_t)g * a.n_parents + f.parent) * a.width + f.full];
 }
 
+// A table's entry that names no page.
+__device__ __forceinline__ bool lacks(const PoolArgs& a, int32_t id) { return (uint32_t)id >= a.n_pages; }
+
 // Entries [c0, c1) of a table row: the ones in them that name no page are wanted.
 __device__ __forceinline__ void range_of(const PoolArgs& a, uint32_t r, uint32_t& c0, uint32_t& c1, bool& fine) {
   const uint32_t have = a.have[r], want = a.want[r], P = a.page_tokens;
@@ -153,13 +156,13 @@ __device__ uint32_t wanted(const PoolArgs& a, uint32_t r, uint32_t g) {
     if (c1 - c0 <= kShort) {
 #pragma unroll
       for (uint32_t i = 0; i < kShort; ++i)
-        if (c0 + i < c1) n += row[c0 + i] < 0;
+        if (c0 + i < c1) n += lacks(a, row[c0 + i]);
     }
     for (uint64_t m = __ballot(c1 - c0 > kShort); m; m &= m - 1) {
       const uint32_t lane = (uint32_t)__builtin_ctzll(m), who = __shfl(r, lane), b0 = __shfl(c0, lane), b1 = __shfl(c1, lane);
       const int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + who) * a.width;
       uint32_t k = 0;
-      for (uint32_t c = b0 + (threadIdx.x & 63); c < b1; c += 64) k += theirs[c] < 0;
+      for (uint32_t c = b0 + (threadIdx.x & 63); c < b1; c += 64) k += lacks(a, theirs[c]);
       for (uint32_t d = 1; d < 64; d *= 2) k += __shfl_xor(k, d);
       if ((threadIdx.x & 63) == lane) n = k;
     }
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
           uint32_t from = at[g];
 #pragma unroll
           for (uint32_t i = 0; i < kShort; ++i)
-            if (c0 + i < c1 && row[c0 + i] < 0) {
+            if (c0 + i < c1 && lacks(a, row[c0 + i])) {
               const int32_t p = list[from++];
               row[c0 + i] = p;
               refs[p] = 1;
@@ -306,9 +309,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_pool_plan(PoolArgs a) {
           uint32_t from = __shfl(at[g], who);
           int32_t* theirs = a.out_tables + ((uint64_t)g * a.n + __shfl(r, who)) * a.width;
           for (uint32_t c = b0; c < b1; c += 64) {
-            const bool lacks = c + lane < b1 && theirs[c + lane] < 0;
-            const uint64_t all = __ballot(lacks);
-            if (lacks) {
+            const bool wants = c + lane < b1 && lacks(a, theirs[c + lane]);
+            const uint64_t all = __ballot(wants);
+            if (wants) {
               const int32_t p = list[from + lanes_below(all)];
               theirs[c + lane] = p;
               refs[p] = 1;
