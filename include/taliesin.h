@@ -625,7 +625,9 @@ int tl_attend_tree(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_bat
 /* ---- pages of a cache ---------------------------------------------------------
  * Requests that branch (several answers to one prompt, beams) share the pages that
  * they have in common. These calls work on whole pages of every layer at once, of
- * contexts of any type; each layer uses the tables of its group.
+ * contexts of any type; each layer uses the tables of its group. What a call writes
+ * (tables, lengths, d_status, the pool's counts, the workspace) must share no byte with
+ * anything else that it is given (TL_EINVAL).
  *
  * A pool counts how many table rows name each page; a page that none names is free.
  * Counts start as the caller sets them (0 for free pages; a page that must never be
@@ -654,8 +656,8 @@ int tl_pages_copy(const tl_ctx* ctx, void* stream, const tl_cache* cache, size_t
  * d_kv_len[parent] tokens on the pages of its table row (device
  * [n_groups][n_parents][table_width]). It shares the parent's full pages (each counts one
  * more owner), and gets a page of its own for the last one if that is partly filled,
- * with a copy of its rows. Its row of d_tables_out (device [n_groups][n][table_width],
- * not overlapping d_tables) names these and -1 behind them; d_len_out[i] is its length.
+ * with a copy of its rows. Its row of d_tables_out (device [n_groups][n][table_width])
+ * names these and -1 behind them; d_len_out[i] is its length.
  * Entries of the parent's that name no page stay -1. d_status (device [n] or NULL):
  * TL_ACCEPT; TL_BADARG for a parent outside [0, n_parents) or longer than its row;
  * TL_MISSING where the pool has no page for it, as tl_pool says (both: a row of -1,
@@ -693,8 +695,8 @@ size_t tl_pages_workspace_bytes(const tl_ctx* ctx, size_t n, size_t n_pages);
  * pages a row's values are written as tl_append writes them (from the first row on that
  * moves): a code is moved as it is where the scales agree, and rounded again where they
  * do not. What lies behind the last kept token is not defined. Pages that a kept token
- * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs], apart
- * from the arrays that are read) becomes the request's length. d_status (device [n_reqs] or NULL):
+ * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs]) becomes
+ * the request's length. d_status (device [n_reqs] or NULL):
  * TL_ACCEPT, or TL_BADARG where an entry is not larger than the one before, names no new
  * token, or needs a page that the tables do not name: the tokens before that entry are
  * kept, in all layers, and d_len_out says how many; or where d_kv_len is less than the

@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "internal.h"
 
@@ -40,14 +41,31 @@ int check_pages(const tl_ctx* ctx, const tl_cache* c) {
 
 bool words_ok(const void* p) { return p && !((uintptr_t)p & 3); }
 bool maybe_words(const void* p) { return !((uintptr_t)p & 3); }
-bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
-  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+// Arrays of a call. What a kernel writes may share no byte with another one: its threads
+// read and write in no particular order.
+struct Bytes {
+  const void* p;
+  uint64_t n;
+};
+bool apart(std::initializer_list<Bytes> written, std::initializer_list<Bytes> read) {
+  auto share = [](const Bytes& a, const Bytes& b) {
+    return a.p && b.p && a.n && b.n && (uintptr_t)a.p < (uintptr_t)b.p + b.n && (uintptr_t)b.p < (uintptr_t)a.p + a.n;
+  };
+  for (const Bytes* a = written.begin(); a != written.end(); ++a) {
+    for (const Bytes* b = a + 1; b != written.end(); ++b)
+      if (share(*a, *b)) return false;
+    for (const Bytes& b : read)
+      if (share(*a, b)) return false;
+  }
+  return true;
 }
 
 int check_pool(const tl_pool* p) {
   if (!p || !words_ok(p->d_refs) || p->n_pages < 0 || p->n_pages > 0x7fffffff) return TL_EINVAL;
   return TL_OK;
 }
+
+Bytes pool_bytes(const tl_ctx* ctx, const tl_pool* p) { return {p->d_refs, 4ull * ctx->geo.n_groups * (uint64_t)p->n_pages}; }
 
 // Table rows of a call: their entries are counted in 32 bits.
 int check_table_rows(uint64_t n, uint64_t width) {
@@ -211,11 +229,12 @@ int tl_pages_fork(const tl_ctx* ctx, void* stream, const tl_pool* pool, const tl
   if (!words_ok(d_parent) || !words_ok(d_len_out) || (n_parents && !words_ok(d_kv_len))) return TL_EINVAL;
   const uint64_t row = 4ull * ctx->geo.n_groups * table_width;
   if (table_width && (!words_ok(d_tables_out) || (n_parents && !words_ok(d_tables)))) return TL_EINVAL;
-  if (overlap(d_tables_out, n * row, d_tables, n_parents * row) || overlap(d_len_out, 4 * n, d_kv_len, 4 * n_parents) ||
-      overlap(d_len_out, 4 * n, d_parent, 4 * n))
-    return TL_EINVAL;
   if (!d_workspace || ((uintptr_t)d_workspace & 15)) return TL_EINVAL;
-  if (workspace_bytes < tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages)) return TL_ERANGE;
+  const uint64_t need = tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages);
+  if (!apart({{d_tables_out, n * row}, {d_len_out, 4 * n}, {d_status, n}, pool_bytes(ctx, pool), {d_workspace, need}},
+             {{d_kv_len, 4 * n_parents}, {d_tables, n_parents * row}, {d_parent, 4 * n}}))
+    return TL_EINVAL;
+  if (workspace_bytes < need) return TL_ERANGE;
   return tl::launch_pages_fork(ctx, stream, pool, cache, n_parents, d_kv_len, d_tables, n, d_parent, d_len_out,
                                d_tables_out, table_width, d_status, d_workspace);
 }
@@ -229,7 +248,10 @@ int tl_pages_take(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n
   if (!n) return TL_OK;
   if (!words_ok(d_have) || !words_ok(d_want) || (table_width && !words_ok(d_tables))) return TL_EINVAL;
   if (!d_workspace || ((uintptr_t)d_workspace & 15)) return TL_EINVAL;
-  if (workspace_bytes < tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages)) return TL_ERANGE;
+  const uint64_t need = tl::pages_workspace(ctx, n, (uint64_t)pool->n_pages), row = 4ull * ctx->geo.n_groups * table_width;
+  if (!apart({{d_tables, n * row}, {d_status, n}, pool_bytes(ctx, pool), {d_workspace, need}}, {{d_have, 4 * n}, {d_want, 4 * n}}))
+    return TL_EINVAL;
+  if (workspace_bytes < need) return TL_ERANGE;
   return tl::launch_pages_take(ctx, stream, pool, n, d_have, d_want, d_tables, table_width, d_status, d_workspace);
 }
 
@@ -240,6 +262,7 @@ int tl_pages_free(const tl_ctx* ctx, void* stream, const tl_pool* pool, size_t n
   if (r || (r = check_table_rows(n, table_width))) return r;
   if (!n || !table_width) return TL_OK;
   if (!words_ok(d_tables) || !maybe_words(d_first) || !maybe_words(d_end)) return TL_EINVAL;
+  if (!apart({{d_tables, 4 * n * ctx->geo.n_groups * table_width}, pool_bytes(ctx, pool)}, {{d_first, 4 * n}, {d_end, 4 * n}})) return TL_EINVAL;
   return tl::launch_pages_free(ctx, stream, pool, n, d_tables, table_width, d_first, d_end);
 }
 
@@ -252,8 +275,9 @@ int tl_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32
   if (!words_ok(batch->d_row_off) || !words_ok(batch->d_kv_len)) return TL_EINVAL;
   if (!words_ok(d_n_keep) || !words_ok(d_len_out) || (batch->n_rows && !words_ok(d_keep))) return TL_EINVAL;
   const uint64_t lens = 4 * batch->n_reqs;
-  if (overlap(d_len_out, lens, batch->d_kv_len, lens) || overlap(d_len_out, lens, d_n_keep, lens) ||
-      overlap(d_len_out, lens, batch->d_row_off, lens + 4) || overlap(d_len_out, lens, d_keep, 4 * batch->n_rows))
+  if (!apart({{d_len_out, lens}, {d_status, batch->n_reqs}},
+             {{batch->d_kv_len, lens}, {batch->d_row_off, lens + 4}, {d_n_keep, lens}, {d_keep, 4 * batch->n_rows},
+              {batch->d_tables, lens * ctx->geo.n_groups * batch->table_width}}))
     return TL_EINVAL;
   return tl::launch_keep(ctx, stream, batch, d_n_keep, d_keep, cache, d_len_out, d_status);
 }
