@@ -635,28 +635,51 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     // window takes four, one after another.
     if (a.step == 1 && a.b.n_rows > (1u << 22)) a.step = 4;
     a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
-    // Fragments that begin in one window are written one after another, so few windows are made
-    // shorter, but not much shorter than long fragments, as each of them takes a place to find that it
-    // is empty. us with two rows a window at least / 64 where fragments are longer: one request of 3,000
-    // tokens on pages of 256, 16 heads of 128, 214 / 36, 24 of 300 226 / 73. 96 requests of 24 rows on pages
-    // of 16 take 18 with shorter windows and 22 without.
-    const uint32_t rows = a.step, R = 64 / (ctx->D / 16);
-    while (a.step > (rows > 64 ? 64 : 2) && a.n_windows < 256) {
-      a.step = (a.step + 1) / 2;
-      a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
+    // Heads that a fragment's workgroup takes at once, and not one round after another
+    // (put_fragment).
+    const uint32_t rows = a.step, R = 64 / (ctx->D / 16), whole = a.n_windows;
+    auto at_once = [&](uint32_t step) {
+      const uint32_t held = step <= R || (a.n_windows >= 256 && step <= kWaves * R) ? 1 : 2;
+      uint32_t span = 1, share = 1;
+      while (span < rows && span < R) span *= 2;
+      while (share < kWaves && held * span * share < rows) share *= 2;
+      return kWaves / share * (R / span);
+    };
+    auto split = [&](uint32_t workgroups, uint32_t heads) {
+      a.splits = std::max(1u, std::min(workgroups / a.n_windows, (ctx->H + heads - 1) / heads));
+      return (ctx->H + a.splits - 1) / a.splits;
+    };
+    // Fragments that begin in one window are written one after another. Shorter windows part them,
+    // but each window that is left empty takes a workgroup the time to find that out, for each
+    // share of the heads. So windows are either whole, and few of them give their heads to several
+    // workgroups, at least four heads to each; or shorter, 256 or more of them, and each
+    // workgroup takes as many heads as it can at once. us, whole / shorter, 8 heads of 128 and pages of 16
+    // unless said. Shorter where all fragments are on the device at the same time:
+    //   3 requests of 40 rows 11.1 / 6.1, 12 of 24 15.5 / 9.0, 12 of 8 8.6 / 8.5 (48 of 8 9.0 / 9.5);
+    // where a fragment has more than 64 rows, and a workgroup much to do for it:
+    //   pages of 128, 1 of 4,096 49 / 24, 1 of 8,192 51 / 42 (1 of 16,384 62 / 82); pages of 256, 16 heads,
+    //   1 of 3,000 94 / 28, 24 of 300 115 / 57, 1 of 8,192 107 / 101 (1 of 16,384 152 / 241, 1 of 24,573 193 / 397);
+    // and where several requests longer than a page begin and end inside pages, so that
+    // there are a fifth more fragments than windows:
+    //   48 of 40 17.7 / 14.7, 96 of 24 18.6 / 14.8, 130 of 20 18.5 / 17.3 (192 of 20 21.3 / 22.2; and 48 of 32 12.6 / 15.0).
+    // Whole in all else: 1 of 3,200 15.4 / 18.7, 1 of 8,192 25.3 / 28.3, 96 of 16 12.7 / 15.4; 16 heads, 1 of 512
+    // 11.5 / 15.7, 1 of 1,552 14.5 / 22.5; pages of 64, 48 of 40 22.1 / 29.8, 16 heads, 1 of 4,096 31.9 / 52.2.
+    const uint64_t fragments = (a.b.n_rows + batch->n_reqs * (ctx->P - 1)) / ctx->P;
+    const uint32_t most = at_once(rows);
+    const uint64_t shares = fragments * ((ctx->H + most - 1) / most);
+    const bool few = shares < 128 || (rows > 64 && shares < 850 && whole < 128);
+    const bool ragged = per > ctx->P && rows <= 64 && 5 * fragments >= 6 * (uint64_t)whole && whole < 256;
+    if (few || ragged) {
+      while (a.step > (rows > 64 ? 64 : 2) && a.n_windows < 256) {
+        a.step = (a.step + 1) / 2;
+        a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
+      }
+      const uint32_t heads = at_once(a.step);
+      a.split_heads = std::min(ctx->H, (split(1100, heads) + heads - 1) / heads * heads);
+    } else {
+      const uint32_t many = a.step > 64 ? 1024 : 512;
+      a.split_heads = a.step > 1 && whole < many ? split(many + whole - 1, std::max<uint32_t>(kWaves, most)) : ctx->H;
     }
-    // A window's heads go to several workgroups, up to about 1,100 in all (half of which have no
-    // fragment): each to so many heads as its wavefronts take at once, not one round after another (put_fragment).
-    // us with four heads each, up to 512 workgroups / with this: 12 requests of up to 24 rows, 8 heads of 128 on pages of
-    // 16, with norms 14 / 11, 40 15 / 12, 96 21 / 21; 3 of 16 rows, 16 heads 9.4 / 7.5; 24,573 tokens on pages of 256
-    // 410 / 345 (up to 2,200 workgroups 410).
-    const uint32_t held = a.step <= R || (a.n_windows >= 256 && a.step <= kWaves * R) ? 1 : 2;
-    uint32_t span = 1, share = 1;
-    while (span < rows && span < R) span *= 2;
-    while (share < kWaves && held * span * share < rows) share *= 2;
-    const uint32_t at_once = kWaves / share * (R / span);
-    a.splits = std::max(1u, std::min(1100 / a.n_windows, (ctx->H + at_once - 1) / at_once));
-    a.split_heads = std::min(ctx->H, ((ctx->H + a.splits - 1) / a.splits + at_once - 1) / at_once * at_once);
     a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
   }
   const uint32_t single = !fp8 || q || d_status ? (a.b.n_rows + kWaves - 1) / kWaves : 0;
