@@ -662,23 +662,30 @@ int launch_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
     // and where several requests longer than a page begin and end inside pages, so that
     // there are a fifth more fragments than windows:
     //   48 of 40 17.7 / 14.7, 96 of 24 18.6 / 14.8, 130 of 20 18.5 / 17.3 (192 of 20 21.3 / 22.2; and 48 of 32 12.6 / 15.0).
-    // Whole in all else: 1 of 3,200 15.4 / 18.7, 1 of 8,192 25.3 / 28.3, 96 of 16 12.7 / 15.4; 16 heads, 1 of 512
+    // Requests of up to 32 rows and no longer than a page are in between: of equal lengths one or
+    // two begin in a window, of different lengths, which only the device has, many may. They get
+    // windows of half of that, or where that leaves few a quarter: 96 of 1 to 24 rows 24.0 / 15.9 (as short as above
+    // 13.1), 192 of 1 to 16 21.4 / 16.1, 96 of 12 each 12.2 / 13.1 (14.9), 130 of 16 each 14.2 / 15.8 (18.5).
+    // Whole in all else: 1 of 3,200 15.4 / 18.7, 1 of 8,192 25.3 / 28.3; 16 heads, 1 of 512
     // 11.5 / 15.7, 1 of 1,552 14.5 / 22.5; pages of 64, 48 of 40 22.1 / 29.8, 16 heads, 1 of 4,096 31.9 / 52.2.
     const uint64_t fragments = (a.b.n_rows + batch->n_reqs * (ctx->P - 1)) / ctx->P;
     const uint32_t most = at_once(rows);
     const uint64_t shares = fragments * ((ctx->H + most - 1) / most);
     const bool few = shares < 128 || (rows > 64 && shares < 850 && whole < 128);
     const bool ragged = per > ctx->P && rows <= 64 && 5 * fragments >= 6 * (uint64_t)whole && whole < 256;
+    const bool several = batch->n_reqs > 1 && per <= ctx->P && rows <= 32 && whole < 256;
+    auto shorten = [&] {
+      a.step = (a.step + 1) / 2;
+      a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
+    };
     if (few || ragged) {
-      while (a.step > (rows > 64 ? 64 : 2) && a.n_windows < 256) {
-        a.step = (a.step + 1) / 2;
-        a.n_windows = (a.b.n_rows + a.step - 1) / a.step;
-      }
+      while (a.step > (rows > 64 ? 64 : 2) && a.n_windows < 256) shorten();
       const uint32_t heads = at_once(a.step);
       a.split_heads = std::min(ctx->H, (split(1100, heads) + heads - 1) / heads * heads);
     } else {
-      const uint32_t many = a.step > 64 ? 1024 : 512;
-      a.split_heads = a.step > 1 && whole < many ? split(many + whole - 1, std::max<uint32_t>(kWaves, most)) : ctx->H;
+      for (int i = 0; several && i < 2 && a.step > 2 && (i == 0 || a.n_windows < 150); ++i) shorten();
+      const uint32_t many = rows > 64 ? 1024 : 512;
+      a.split_heads = rows > 1 && a.n_windows < many ? split(many + a.n_windows - 1, std::max<uint32_t>(kWaves, most)) : ctx->H;
     }
     a.splits = (ctx->H + a.split_heads - 1) / a.split_heads;
   }

@@ -20,6 +20,9 @@ SIDES = [  # P, H, D, q_len, held
     (16, 16, 64, [16] * 100, 7),      # and no longer
     (16, 16, 64, [5] * 300, 3),       # heads of which a workgroup takes four, or all, at once
     (16, 16, 64, [2] * 520, 3),
+    (16, 8, 128, [1 + i * 7 % 24 for i in range(96)], 5),   # lengths that differ
+    (64, 8, 128, [1 + i * 11 % 50 for i in range(40)], 9),
+    (16, 4, 256, [1 + i * 5 % 14 for i in range(130)], 1),
 ]
 
 
