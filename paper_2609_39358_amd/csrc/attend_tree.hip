@@ -417,18 +417,25 @@ Shape rows_shape(const tl_ctx* ctx, uint32_t n_q_heads, uint64_t n_reqs, uint64_
   return s;
 }
 
-// Whether each tile goes to one workgroup as a whole. Where a layer has a window, tiles have
-// about as many keys (the window's and the new ones), and if they fill the workgroups, in some
-// rounds, to a good part, there is little to even out: no tile is started and ended twice, no parts are written,
-// and there is no join. us, cut / whole, window of 1,024, 16 heads of 128, bf16, requests of 77 tokens (16
+// Whether each tile goes to one workgroup as a whole. Where a layer has a window, no tile has more
+// keys than that and the new tokens, and if the tiles fill the workgroups, in some rounds, to a good
+// part, there is little to even out: no tile is started and ended twice, no parts are written, and
+// there is no join. us, cut / whole, window of 1,024, 16 heads of 128, bf16, requests of 77 tokens (16
 // tiles each, 256 workgroups): 8 requests 75 / 68, 10 81 / 69, 12 93 / 73, 16 101 / 77, 17 108 / 133, 24 142 / 135, 32
 // 172 / 143; of 30 tokens (512 workgroups) 32 requests 102 / 82, 44 166 / 156, 60 246 / 213; of 12
-// (k_attend_rows, 4 tiles each) 44 104 / 88, 64 138 / 119, 110 220 / 201; 16 of 1 to 77 tokens 96 / 100. (Without a
-// window the lengths, which only the device has, may differ by any factor.)
+// (k_attend_rows, 4 tiles each) 44 104 / 88, 64 138 / 119, 110 220 / 201; 16 of 1 to 77 tokens 96 / 100.
+// But the lengths, which only the device has, may differ by any factor, and then the longest tile
+// is what a call waits for: so the window is a small one, of 2,048 keys with the new tokens. Where one
+// request is longer than the window and all others have some tokens more than are new, 16 of 77 tokens
+// take, with a window of 512 58 / 54, of 1,024 57 / 67, of 2,048 63 / 93, of 16,384 108 / 464 (64 of 12 tokens
+// 42 / 36, 47 / 53, 47 / 87, 85 / 569); with lengths that differ less (log-normal, 1,500 in the middle) 75 / 55, 90 / 63,
+// 104 / 88, 195 / 469 (79 / 58, 136 / 99, 181 / 157, 297 / 739).
+constexpr uint64_t kWholeKeys = 2048;
+
 bool whole_tiles(const tl_ctx* ctx, uint32_t layer, const Shape& s, const Kind& k, uint64_t n_reqs, uint64_t n_rows) {
   const uint64_t tokens = (n_rows + n_reqs - 1) / n_reqs, tiles = n_reqs * k.heads * ((tokens + k.tile_rows - 1) / k.tile_rows);
   const uint64_t rounds = (tiles + s.workers - 1) / s.workers;
-  return ctx->window[layer] && tiles * 5 >= rounds * s.workers * 3;
+  return ctx->window[layer] && ctx->window[layer] + tokens <= kWholeKeys && tiles * 5 >= rounds * s.workers * 3;
 }
 
 }  // namespace
