@@ -796,25 +796,25 @@ __device__ __forceinline__ void segment16(const AttendArgs& a, Lds16<D, WAVES>& 
 // Tiles of 16 rows for all requests. One token over 97,000 in scaled pages of 16
 // heads of 128: 78 us, 5.1 TB/s (a large copy reaches 4.7); 64 requests of up to
 // 32,768 164 us, 5.2 TB/s.
-template <int D, bool FP8, bool EVEN, int MODE>
+template <int D, bool FP8, bool EVEN>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend16(AttendArgs a) {
   __shared__ union {
     PlanLds plan;
     Lds16<D, 4> s;
   } l;
   Cursor cur;
-  const bool any = plan<MODE>(a, l.plan, cur);
+  const bool any = plan<kText>(a, l.plan, cur);
   if (!any) {
     if (threadIdx.x == 0) ((GlobalShare)a.share)[cur.worker].parts = 0;
     return;
   }
   Request q = uniform(request_of(a, cur.r));
   for (bool first = true; cur.at < cur.end; first = false) {
-    const Span s = span_of<MODE>(a, q, cur.tile);
+    const Span s = span_of<kText>(a, q, cur.tile);
     uint32_t k0, k1;
-    const uint64_t tile_end = blocks_of<MODE>(a, cur, q, s, k0, k1);
+    const uint64_t tile_end = blocks_of<kText>(a, cur, q, s, k0, k1);
     if (first && threadIdx.x == 0) note_share(a, cur, q, s, k0, k1);
-    if (k0 < k1) segment16<D, FP8, EVEN, 4, MODE>(a, l.s, cur, q, s, k0, k1);
+    if (k0 < k1) segment16<D, FP8, EVEN, 4, kText>(a, l.s, cur, q, s, k0, k1);
     cur.at = min(cur.end, tile_end);
     if (cur.at == tile_end) {
       cur.first = tile_end;

@@ -31,7 +31,7 @@ int launch_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batc
       if (sh.waves)
         launch_many<D(), fp8(), even(), kText>(sh, s, a);
       else
-        hipLaunchKernelGGL((k_attend16<D(), fp8(), even(), kText>), dim3(sh.workers), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_attend16<D(), fp8(), even()>), dim3(sh.workers), dim3(256), 0, s, a);
     }
     launch_join<D()>(sh, s, a);
   });

@@ -82,7 +82,6 @@ __global__ __launch_bounds__(kThreads) void k_pages_copy(CopyArgs a) {
 struct PoolArgs {
   int32_t* refs;  // [n_groups][n_pages]
   uint32_t n_pages, n_groups, page_tokens;
-  FastDiv page;
   uint32_t n;      // requests that want pages
   uint32_t width;  // of a table row
   uint8_t* status;
@@ -902,7 +901,6 @@ void fill_pool(PoolArgs& p, const tl_ctx* ctx, const tl_pool* pool, uint64_t n, 
   p.n_pages = (uint32_t)pool->n_pages;
   p.n_groups = ctx->geo.n_groups;
   p.page_tokens = ctx->P;
-  p.page.set(ctx->P);
   p.n = (uint32_t)n;
   p.width = (uint32_t)width;
   p.status = d_status;
