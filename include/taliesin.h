@@ -565,7 +565,7 @@ int tl_append(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
  * rotated: a head x of head_dim elements becomes x / sqrt(mean(x^2) + eps) times its
  * weights, with TL_NORM_CENTER less its mean first, in 32-bit arithmetic; nothing is
  * rounded to 16 bits between the norm and the rotation. Values are not normed. norm NULL:
- * tl_append. */
+ * tl_append. (Not here: a bias after the weights, and norms over all heads together.) */
 #define TL_NORM_CENTER 1
 typedef struct tl_norm {
   const float* d_q_weight; /* device, 16-byte aligned: head h's head_dim weights begin at   */
@@ -588,7 +588,8 @@ int tl_append_norm(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_bat
  * id is outside [0, n_pages), such as -1 for pages that were not restored, are
  * left out, and what a page holds past the request's keys is not used. A row
  * that sees no key gets zeros. d_lse (device [n_rows][n_q_heads] floats, or
- * NULL) gets log(sum_j w_j), minus infinity for such a row.
+ * NULL) gets log(sum_j w_j), minus infinity for such a row. For their product with
+ * the values the w_j are rounded to bf16, as out is; sums are in 32 bits.
  * Keys and values that are NaN or infinite reach the rows that see them, and no
  * others; a query that is NaN reaches its own row. A row whose scores are all
  * minus infinity gets zeros, as if it saw no key.
@@ -609,7 +610,8 @@ int tl_attend(const tl_ctx* ctx, void* stream, uint32_t layer, const tl_batch* b
  * tokens past the mask's words are not seen. A row sees itself only if its mask says so,
  * and the masks alone decide about new tokens, whatever their positions. In all else
  * tl_attend: results, d_lse, rows that see nothing, missing pages, values that are not
- * finite, workspace (tl_attend_workspace_bytes) and kernels. The rows are appended in the
+ * finite, workspace (tl_attend_workspace_bytes) and kernels. As there, the w_j are rounded
+ * to bf16 for their product with the values, and not for their sum. The rows are appended in the
  * tree's order with their depths as positions (tl_rope.d_pos); after a choice of tokens
  * tl_keep moves those that stay together. */
 typedef struct tl_tree {
@@ -694,14 +696,18 @@ size_t tl_pages_workspace_bytes(const tl_ctx* ctx, size_t n, size_t n_pages);
  * tokens that were accepted; the first and last tokens of a long request). On scaled
  * pages a row's values are written as tl_append writes them (from the first row on that
  * moves): a code is moved as it is where the scales agree, and rounded again where they
- * do not. What lies behind the last kept token is not defined. Pages that a kept token
+ * do not. So a page that was partly filled before, or whose first new tokens stay where they
+ * are, keeps its scale if that is the larger one, also where a token that is not kept has
+ * raised it. What lies behind the last kept token is not defined. Pages that a kept token
  * lies on or moves to must be the request's own. d_len_out[r] (device [n_reqs]) becomes
- * the request's length. d_status (device [n_reqs] or NULL):
- * TL_ACCEPT, or TL_BADARG where an entry is not larger than the one before, names no new
- * token, or needs a page that the tables do not name: the tokens before that entry are
- * kept, in all layers, and d_len_out says how many; or where d_kv_len is less than the
- * request's rows or more than its table row holds: nothing moves, and d_len_out is
- * d_kv_len. One kernel, no workspace. */
+ * the request's length. d_status (device [n_reqs] or NULL): TL_ACCEPT, or TL_BADARG where
+ * an entry is not larger than the one before, names no new token, or moves from or to a
+ * page that the tables do not name: the tokens before that entry are kept, in all layers,
+ * and d_len_out says how many; or where d_kv_len is less than the request's rows or more
+ * than its table row holds: nothing moves, and d_len_out is d_kv_len. One kernel, no
+ * workspace; which one follows from the batch's rows per request on average, so that a
+ * request of many thousands of rows is better kept in a call of its own, apart from
+ * those of a few. */
 int tl_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const uint32_t* d_n_keep, const uint32_t* d_keep,
             const tl_cache* cache, uint32_t* d_len_out, uint8_t* d_status);
 

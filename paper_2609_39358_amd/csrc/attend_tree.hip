@@ -148,7 +148,7 @@ __device__ __forceinline__ void block_rows(const AttendArgs& a, const u32x4 (*qs
     for (int i = 0; i < N; ++i) {
       const float y = exp2_(__builtin_fmaf(x[g][i], a.scale, -r.s[g].top));
       r.s[g].sum += y;
-      w[g][i / 8][i % 8] = (__bf16)y;
+      w[g][i / 8][i % 8] = (__bf16)y;  // for the product, which takes bf16; the result is no finer
     }
 #pragma unroll
   for (int k = 0; k < Tile::kGroups; ++k)

@@ -996,6 +996,9 @@ int launch_keep(const tl_ctx* ctx, void* stream, const tl_batch* batch, const ui
   a.len_out = d_len_out;
   a.status = d_status;
   a.columns = a.c.row_bytes / 16;
+  // By the average, as the lengths are on the device only: a request of thousands of rows among
+  // many of a few is walked by single wavefronts, some rows a step. One of 20,011 that keeps 8,003
+  // beside 96 of up to 48, 24 slabs of 16 heads of 128 in 8 bits: 5.5 ms, in calls of their own 0.47 and 0.03.
   const bool many = batch->n_rows / batch->n_reqs > 256;
   hipStream_t s = (hipStream_t)stream;
   (void)hipGetLastError();

@@ -380,7 +380,10 @@ class NewTokens:
     Drafted tokens: with d_seen i64 [n_rows, words] the rows of a request are a tree
     and see each other by their masks (tl_tree), and d_pos i32 [n_rows] are their
     positions, for the rotation and for windows. keep() moves the accepted ones
-    together once all layers are done."""
+    together once all layers are done.
+
+    Pairs are halves of a head and positions have one axis: models that turn adjacent
+    pairs, or have several axes, call tl_append and tl_attend with a make_rope of theirs."""
 
     def __init__(self, ctx: T.Ctx, cache: PagedCache, n_q_heads: int, n_rows: int, d_row_off, d_kv_len, d_tables,
                  d_cos_sin=None, stream=None, d_seen=None, d_pos=None):
